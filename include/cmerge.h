@@ -21,6 +21,10 @@
  * the paper's baselines over the same render:
  *   cm_multiset_order       the naive re-render order of §5.9 (no dedupe)
  *   cm_bag_plan             BagMerge with a caller-supplied order (§4.2)
+ * to serve a merged cache:
+ *   cm_qcache_tables        block tables and slots of a step from the lengths
+ *   cm_qcache_write         K and V rows into a cache held in 8 bits on pages
+ *   cm_qcache_attention     attention of a step's queries over that cache
  * and, to run step 1 without a second read of the fragments:
  *   cm_equal_key_mask       the deliveries whose digest the order needs
  *   cm_fragment_hash_select the Id of a subset of the deliveries
@@ -486,6 +490,125 @@ int32_t cm_paged_deliveries(const cm_pagedset* set, int32_t routing_layer, int64
                             void* workspace, size_t workspace_bytes, void* stream);
 int32_t cm_paged_workspace_size(const cm_pagedset* set, size_t* bytes_out);
 
+/* ---------------------------------------------------------------- serving a merged cache
+ * A merged cache (or any KV cache) held in 8 bits on pages, and what a serving
+ * loop does with it: cm_qcache_tables at the start of a step, cm_qcache_write and
+ * cm_qcache_attention in each layer. All three take their lengths from device
+ * memory, so a loop needs no host round trip and its calls can be captured into
+ * a HIP graph.
+ *
+ * codes_dev: [L][2][P][H][B][d] bytes, each an OCP e4m3 number (4 exponent bits, 3
+ * mantissa bits, no infinity); page p of layer l's K is the [H][B][d] block at byte
+ * (2l * P + p) * H * B * d, its V at ((2l + 1) * P + p) * H * B * d: the layout of
+ * cm_pagedset's pool. scales_dev: [L][2][P][H] fp32, one for the B tokens of a page
+ * and a head. A stored value is code * scale. d is 64, 128 or 256; B is 16, 32, 64
+ * or 128; codes_dev is 16-byte, scales_dev 4-byte aligned.
+ * A token's slot is page * B + its row in the page. */
+#define CM_QCACHE_MAX_REQUESTS 1024
+typedef struct {
+  int32_t L;
+  int32_t H;
+  int32_t d;
+  int32_t block;     /* B, tokens per page */
+  int64_t pages;     /* P */
+  void* codes_dev;
+  float* scales_dev;
+} cm_qcache;
+
+/* Block tables and slot maps of a step from the requests' lengths. Request r
+ * holds held_dev[r] tokens and brings new_dev[r] more (either may be 0). Row r of
+ * table_dev (n rows of table_width int32) names the pages of its tokens in order:
+ * the first ceil(held / B) entries are kept, the entries up to ceil((held + new) / B)
+ * are taken from free_dev (n_free int32 page ids) in the order of the requests, later
+ * entries are not touched. The step's tokens are the requests' new tokens one after
+ * another, n_tokens in all: slots_dev[i] is the slot of token i, or -1 where its table
+ * entry is not a page in [0, pages). rows_dev (n + 1 int32): exclusive prefix sums of
+ * new; lens_dev (n int32): held + new. info_dev (4 int64): status, tokens, pages
+ * taken, the longest length. Status CM_EINVAL means a length is negative, the sum of
+ * new is not n_tokens, a request is longer than its table row, or the free list is
+ * too short (info_dev[2] then holds the pages needed): no table entry is written,
+ * every slot is -1, rows_dev is 0 and lens_dev is held (0 where that is negative), so
+ * that the calls below do nothing for the step. The call itself returns CM_OK.
+ * 1 <= n <= CM_QCACHE_MAX_REQUESTS; slots_dev and info_dev are 8-byte aligned, the
+ * others 4-byte. */
+int32_t cm_qcache_tables(int64_t pages, int32_t block, int32_t n, const int32_t* held_dev,
+                         const int32_t* new_dev, const int32_t* free_dev, int64_t n_free,
+                         int32_t* table_dev, int64_t table_width, int64_t n_tokens,
+                         int64_t* slots_dev, int32_t* rows_dev, int32_t* lens_dev,
+                         int64_t* info_dev, void* stream);
+
+/* K or V rows of a step: row t of head h of the l-th layer written starts at element
+ * l * layer_stride + t * token_stride + h * head_stride of data and holds d
+ * consecutive elements. data is 16-byte aligned and the strides are multiples of 16
+ * bytes. (A merged cache [L][2][1][H][T][d] is layer_stride 2HTd, token_stride d,
+ * head_stride Td.) */
+typedef struct {
+  const void* data_dev;
+  int64_t layer_stride;
+  int64_t token_stride;
+  int64_t head_stride;
+} cm_qrows;
+
+/* Writes n_tokens rows of K and of V for layers [first_layer, first_layer + n_layers)
+ * into their slots (slots_dev: n_tokens int64; a slot outside [0, P * B) is skipped).
+ * The tokens of one page must be consecutive, skipped ones aside, and in ascending
+ * slots, as cm_qcache_tables numbers them; tokens before and after a skipped one are
+ * written as if by two calls. For each page, head, layer and K/V:
+ *   amax  = the greatest finite |x| of the new rows in the page
+ *   scale = the least 2^e, e >= -120, with amax <= 448 * 2^e; if the first new row is
+ *           not row 0, the greater of that and the page's old scale
+ *   code  = x / scale rounded to nearest even (x / scale is exact: the scale is a power
+ *           of two); NaN and infinity become NaN
+ * and where the scale has grown the codes of the rows before the first new one are
+ * multiplied by old / new scale and rounded again. Rows after the last new one are
+ * not touched. dtype: of the rows (cm_dtype). */
+int32_t cm_qcache_write(const cm_qcache* cache, int32_t first_layer, int32_t n_layers,
+                        int32_t dtype, const cm_qrows* k, const cm_qrows* v, int64_t n_tokens,
+                        const int64_t* slots_dev, void* stream);
+
+/* Attention of a step's queries over one layer of the cache. Request r has the
+ * query rows [rows_dev[r], rows_dev[r + 1]) (rows_dev NULL: row r alone, n_rows == n)
+ * and lens_dev[r] tokens in the pages of its table row. Its i-th of c rows stands at
+ * position p = lens - c + i and sees the positions j with max(0, p - window + 1) <= j
+ * <= p (window 0: 0 <= j <= p) whose table entry is a page in [0, P); other entries,
+ * such as -1 for a page that was evicted, hide their tokens. With g = q_heads / H, query
+ * head a reads KV head a / g:
+ *   x_j = scale * q . k_j,  out = sum_j exp(x_j - lse) v_j,  lse = log sum_j exp(x_j)
+ * A row that sees nothing gives out 0 and lse -inf. What a row does not see has no
+ * effect on it, NaN included. Products, exponents and sums are in fp32; out is rounded
+ * once.
+ * q_dev, out_dev: n_rows rows of q_heads heads of d elements of dtype, 16-byte
+ * aligned, strides in elements, multiples of 16 bytes. lse_dev: n_rows * q_heads fp32,
+ * or NULL. max_rows: the most rows a request may have (a request's rows past it are
+ * not computed). A length above table_width * B counts as that. g is at most 64. */
+typedef struct {
+  int32_t n;           /* requests */
+  int32_t q_heads;
+  int32_t dtype;       /* cm_dtype of q and out */
+  int32_t window;      /* 0: none */
+  int64_t n_rows;
+  int32_t max_rows;
+  float scale;
+  const void* q_dev;
+  int64_t q_row_stride;
+  int64_t q_head_stride;
+  void* out_dev;
+  int64_t out_row_stride;
+  int64_t out_head_stride;
+  float* lse_dev;
+  const int32_t* rows_dev;
+  const int32_t* lens_dev;
+  const int32_t* table_dev;
+  int64_t table_width;
+} cm_qattention;
+
+/* Workspace: cm_qcache_attention_size() bytes (n, n_rows, max_rows, q_heads and the
+ * cache's shape decide it, not the lengths). */
+int32_t cm_qcache_attention_size(const cm_qcache* cache, const cm_qattention* step,
+                                 size_t* bytes_out);
+int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qattention* step,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------------------------- timing
  * Optional per-kernel timing with HIP events recorded on the launch stream
  * around every kernel this library enqueues (off by default; a process-wide
@@ -493,7 +616,8 @@ int32_t cm_paged_workspace_size(const cm_pagedset* set, size_t* bytes_out);
  * to the per-kernel totals and returns the total milliseconds and launch count
  * for one kernel name ("hash_prep", "hash_leaf", "hash_parent", "hash_final",
  * "knorm_rows", "knorm_tree", "order", "key_mask", "render_prep", "render",
- * "render_hash", "paged", "paged_hash_render"). "hash_parent" is the trees above the
+ * "render_hash", "paged", "paged_hash_render", "qcache_tables", "qcache_write",
+ * "qcache_attention", "qcache_join"). "hash_parent" is the trees above the
  * stripes that the chunk kernels fold, with the Ids where one launch makes both and
  * where tensors of 2 to 64 chunks leave only the Ids to make; "hash_final" the Ids
  * otherwise. "key_mask" includes the comparison of re-deliveries. */

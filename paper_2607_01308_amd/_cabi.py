@@ -22,6 +22,7 @@ CM_BF16 = 1
 CM_ROPE_HALF = 0
 CM_ROPE_INTERLEAVED = 1
 CM_MAX_FRAGMENTS = 1024
+CM_QCACHE_MAX_REQUESTS = 1024
 NOALLOC_SCRATCH_BYTES = 64 << 20     # CM_NOALLOC_SCRATCH_BYTES
 
 PLAN_STATUS, PLAN_N, PLAN_NUNIQUE, PLAN_TOUT, PLAN_HEADER = 0, 1, 2, 3, 4
@@ -36,6 +37,7 @@ EXPORTS = (
     "cm_graph_launch", "cm_graph_destroy",
     "cm_paged_workspace_size", "cm_paged_order", "cm_paged_hash_select", "cm_paged_tables",
     "cm_paged_render", "cm_paged_render_hash", "cm_paged_deliveries",
+    "cm_qcache_tables", "cm_qcache_write", "cm_qcache_attention_size", "cm_qcache_attention",
     "cm_timing_enable", "cm_timing_reset", "cm_timing_query",
 )
 
@@ -75,6 +77,50 @@ class CmRope(ctypes.Structure):
     _fields_ = [("base", ctypes.c_double), ("style", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class CmQcache(ctypes.Structure):
+    _fields_ = [
+        ("L", ctypes.c_int32),
+        ("H", ctypes.c_int32),
+        ("d", ctypes.c_int32),
+        ("block", ctypes.c_int32),
+        ("pages", ctypes.c_int64),
+        ("codes_dev", ctypes.c_void_p),
+        ("scales_dev", ctypes.c_void_p),
+    ]
+
+
+class CmQrows(ctypes.Structure):
+    _fields_ = [
+        ("data_dev", ctypes.c_void_p),
+        ("layer_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
+class CmQattention(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int32),
+        ("q_heads", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("window", ctypes.c_int32),
+        ("n_rows", ctypes.c_int64),
+        ("max_rows", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("q_dev", ctypes.c_void_p),
+        ("q_row_stride", ctypes.c_int64),
+        ("q_head_stride", ctypes.c_int64),
+        ("out_dev", ctypes.c_void_p),
+        ("out_row_stride", ctypes.c_int64),
+        ("out_head_stride", ctypes.c_int64),
+        ("lse_dev", ctypes.c_void_p),
+        ("rows_dev", ctypes.c_void_p),
+        ("lens_dev", ctypes.c_void_p),
+        ("table_dev", ctypes.c_void_p),
+        ("table_width", ctypes.c_int64),
+    ]
+
+
 class CmError(RuntimeError):
     def __init__(self, status: int, where: str, message: str):
         self.status = status
@@ -95,6 +141,7 @@ def lib() -> ctypes.CDLL:
         P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         FS = ctypes.POINTER(CmFragset)
         PS = ctypes.POINTER(CmPagedset)
+        QC, QR, QA = (ctypes.POINTER(t) for t in (CmQcache, CmQrows, CmQattention))
         sig = {
             "cm_version": (I32, []),
             "cm_last_error": (ctypes.c_char_p, []),
@@ -133,6 +180,10 @@ def lib() -> ctypes.CDLL:
                                            SZ, P]),
             "cm_paged_deliveries": (I32, [PS, I32, I64, ctypes.POINTER(CmRope), P, P, I64, P, P,
                                           P, P, P, P, P, P, SZ, P]),
+            "cm_qcache_tables": (I32, [I64, I32, I32, P, P, P, I64, P, I64, I64, P, P, P, P, P]),
+            "cm_qcache_write": (I32, [QC, I32, I32, I32, QR, QR, I64, P, P]),
+            "cm_qcache_attention_size": (I32, [QC, QA, ctypes.POINTER(SZ)]),
+            "cm_qcache_attention": (I32, [QC, I32, QA, P, SZ, P]),
             "cm_timing_enable": (I32, [I32]),
             "cm_timing_reset": (I32, []),
             "cm_timing_query": (I32, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),

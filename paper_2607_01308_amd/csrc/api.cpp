@@ -5,12 +5,14 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <string>
 #include <vector>
 
 #include "cmerge.h"
 #include "internal.h"
+#include "qcache.h"
 
 namespace {
 
@@ -140,7 +142,7 @@ int64_t min_T(const cm::SetDesc& s) {
 const char* const kKernelNames[cm::K_COUNT] = {
     "hash_prep", "hash_leaf", "hash_parent", "hash_final", "knorm_rows", "knorm_tree",
     "order",     "key_mask",  "render_prep", "render",     "render_hash", "paged",
-    "paged_hash_render"};
+    "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention", "qcache_join"};
 std::atomic<bool> g_timing{false};
 // set while this thread captures a call into a graph: no timing events then
 thread_local bool t_capturing = false;
@@ -1186,6 +1188,227 @@ int32_t cm_paged_render_hash(const cm_pagedset* set, const int64_t* plan_dev,
                                               static_cast<uint8_t*>(workspace),
                                               static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_paged_render_hash");
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ 8-bit paged cache
+namespace {
+
+int32_t check_pages(int64_t pages, int32_t block) {
+  if (block < 16 || block > 128 || !is_pow2(block))
+    return fail(CM_ESHAPE, "block must be 16, 32, 64 or 128, got " + std::to_string(block));
+  if (pages < 1 || pages > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "pages must be in [1, 2^31 - 1], got " + std::to_string(pages));
+  return CM_OK;
+}
+
+int32_t check_qcache(const cm_qcache* c, cm::QCacheDesc* out) {
+  if (!c) return fail(CM_EINVAL, "cache is NULL");
+  if (c->L < 1 || c->H < 1) return fail(CM_EINVAL, "L and H must be >= 1");
+  if ((int64_t)2 * c->L * c->H > 65535) return fail(CM_ESHAPE, "2 * L * H must be <= 65535");
+  if (c->d != 64 && c->d != 128 && c->d != 256)
+    return fail(CM_ESHAPE, "d must be 64, 128 or 256, got " + std::to_string(c->d));
+  int32_t st = check_pages(c->pages, c->block);
+  if (st != CM_OK) return st;
+  if (!c->codes_dev || !aligned(c->codes_dev, 16))
+    return fail(CM_EINVAL, "codes_dev is NULL or not 16-byte aligned");
+  if (!c->scales_dev || !aligned(c->scales_dev, 4))
+    return fail(CM_EINVAL, "scales_dev is NULL or misaligned");
+  out->L = c->L;
+  out->H = c->H;
+  out->d = c->d;
+  out->b_shift = __builtin_ctz((unsigned)c->block);
+  out->pages = c->pages;
+  out->codes = static_cast<uint8_t*>(c->codes_dev);
+  out->scales = c->scales_dev;
+  return CM_OK;
+}
+
+int32_t element_bytes(int32_t dtype, int32_t* out) {
+  if (dtype != CM_F32 && dtype != CM_BF16)
+    return fail(CM_EDTYPE, "dtype must be CM_F32 or CM_BF16, got " + std::to_string(dtype));
+  *out = dtype == CM_F32 ? 4 : 2;
+  return CM_OK;
+}
+
+// Strided rows that the kernels load in 16-byte pieces.
+int32_t check_strides(const char* what, const void* data, int32_t esize,
+                      std::initializer_list<int64_t> strides) {
+  if (!data || !aligned(data, 16))
+    return fail(CM_EINVAL, std::string(what) + " is NULL or not 16-byte aligned");
+  for (int64_t s : strides)
+    if (s < 0 || s > ((int64_t)1 << 40) || (s * esize) % 16 != 0)
+      return fail(CM_EINVAL, std::string(what) + " has a stride that is negative, above 2^40 or "
+                                                 "no multiple of 16 bytes");
+  return CM_OK;
+}
+
+// The part of an attention call that decides its workspace.
+int32_t check_qattention_shape(const cm::QCacheDesc& c, const cm_qattention* s) {
+  if (!s) return fail(CM_EINVAL, "step is NULL");
+  if (s->n < 1 || s->n > CM_QCACHE_MAX_REQUESTS)
+    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
+                               "], got " + std::to_string(s->n));
+  if (s->q_heads < 1 || s->q_heads % c.H != 0 || s->q_heads / c.H > 64)
+    return fail(CM_ESHAPE, "q_heads must be 1 to 64 times H = " + std::to_string(c.H) + ", got " +
+                               std::to_string(s->q_heads));
+  if (s->n_rows < 0 || s->n_rows > 0x7FFFFFFF / s->q_heads)
+    return fail(CM_EINVAL, "n_rows must be in [0, 2^31 / q_heads), got " + std::to_string(s->n_rows));
+  if (s->max_rows < 0) return fail(CM_EINVAL, "max_rows must be >= 0");
+  return CM_OK;
+}
+
+cm::QAttentionPlan qattention_plan(const cm::QCacheDesc& c, const cm_qattention* s) {
+  return cm::plan_qcache_attention(c.H, c.d, s->q_heads / c.H, s->n, s->n_rows);
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t cm_qcache_tables(int64_t pages, int32_t block, int32_t n, const int32_t* held_dev,
+                         const int32_t* new_dev, const int32_t* free_dev, int64_t n_free,
+                         int32_t* table_dev, int64_t table_width, int64_t n_tokens,
+                         int64_t* slots_dev, int32_t* rows_dev, int32_t* lens_dev,
+                         int64_t* info_dev, void* stream) {
+  g_err.clear();
+  int32_t st = check_pages(pages, block);
+  if (st != CM_OK) return st;
+  if (n < 1 || n > CM_QCACHE_MAX_REQUESTS)
+    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
+                               "], got " + std::to_string(n));
+  if (!held_dev || !new_dev || !aligned(held_dev, 4) || !aligned(new_dev, 4))
+    return fail(CM_EINVAL, "held_dev / new_dev NULL or misaligned");
+  if (n_free < 0 || n_free > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_free must be in [0, 2^31), got " + std::to_string(n_free));
+  if (n_free > 0 && (!free_dev || !aligned(free_dev, 4)))
+    return fail(CM_EINVAL, "free_dev is NULL or misaligned");
+  if (table_width < 1 || table_width > ((int64_t)1 << 30) / block)
+    return fail(CM_EINVAL, "table_width must be in [1, 2^30 / block], got " +
+                               std::to_string(table_width));
+  if (!table_dev || !aligned(table_dev, 4)) return fail(CM_EINVAL, "table_dev is NULL or misaligned");
+  if (n_tokens < 0 || n_tokens > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_tokens must be in [0, 2^31), got " + std::to_string(n_tokens));
+  if (n_tokens > 0 && (!slots_dev || !aligned(slots_dev, 8)))
+    return fail(CM_EINVAL, "slots_dev is NULL or misaligned");
+  if (!rows_dev || !lens_dev || !aligned(rows_dev, 4) || !aligned(lens_dev, 4))
+    return fail(CM_EINVAL, "rows_dev / lens_dev NULL or misaligned");
+  if (!info_dev || !aligned(info_dev, 8)) return fail(CM_EINVAL, "info_dev is NULL or misaligned");
+  hipError_t e = cm::launch_qcache_tables(pages, __builtin_ctz((unsigned)block), n, held_dev,
+                                          new_dev, free_dev, n_free, table_dev, table_width,
+                                          n_tokens, slots_dev, rows_dev, lens_dev, info_dev,
+                                          static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_tables");
+}
+
+int32_t cm_qcache_write(const cm_qcache* cache, int32_t first_layer, int32_t n_layers,
+                        int32_t dtype, const cm_qrows* k, const cm_qrows* v, int64_t n_tokens,
+                        const int64_t* slots_dev, void* stream) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c), esize = 0;
+  if (st != CM_OK) return st;
+  if (first_layer < 0 || n_layers < 0 || first_layer > c.L - n_layers)
+    return fail(CM_EINVAL, "layers [first_layer, first_layer + n_layers) must lie in [0, L)");
+  if ((st = element_bytes(dtype, &esize)) != CM_OK) return st;
+  if (n_tokens < 0 || n_tokens > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_tokens must be in [0, 2^31), got " + std::to_string(n_tokens));
+  if (!k || !v) return fail(CM_EINVAL, "k / v is NULL");
+  if (n_tokens == 0 || n_layers == 0) return CM_OK;
+  if ((st = check_strides("k", k->data_dev, esize,
+                          {k->layer_stride, k->token_stride, k->head_stride})) != CM_OK)
+    return st;
+  if ((st = check_strides("v", v->data_dev, esize,
+                          {v->layer_stride, v->token_stride, v->head_stride})) != CM_OK)
+    return st;
+  if (!slots_dev || !aligned(slots_dev, 8)) return fail(CM_EINVAL, "slots_dev is NULL or misaligned");
+  const auto bytes = [&](const cm_qrows* r) {
+    return cm::QRows{static_cast<const uint8_t*>(r->data_dev), r->layer_stride * esize,
+                     r->token_stride * esize, r->head_stride * esize};
+  };
+  hipError_t e = cm::launch_qcache_write(c, first_layer, n_layers, dtype, bytes(k), bytes(v),
+                                         n_tokens, slots_dev, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_write");
+}
+
+int32_t cm_qcache_attention_size(const cm_qcache* cache, const cm_qattention* step,
+                                 size_t* bytes_out) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c);
+  if (st != CM_OK) return st;
+  if ((st = check_qattention_shape(c, step)) != CM_OK) return st;
+  if (!bytes_out) return fail(CM_EINVAL, "bytes_out is NULL");
+  *bytes_out = qattention_plan(c, step).bytes;
+  return CM_OK;
+}
+
+int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qattention* step,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c), esize = 0;
+  if (st != CM_OK) return st;
+  if (layer < 0 || layer >= c.L)
+    return fail(CM_EINVAL, "layer must be in [0, L), got " + std::to_string(layer));
+  if ((st = check_qattention_shape(c, step)) != CM_OK) return st;
+  if ((st = element_bytes(step->dtype, &esize)) != CM_OK) return st;
+  if (step->window < 0) return fail(CM_EINVAL, "window must be >= 0");
+  if (!std::isfinite(step->scale)) return fail(CM_EINVAL, "scale must be finite");
+  if (!step->rows_dev && step->n_rows != step->n)
+    return fail(CM_EINVAL, "without rows_dev there is one row for each request: n_rows == n");
+  if (step->rows_dev && !aligned(step->rows_dev, 4)) return fail(CM_EINVAL, "rows_dev is misaligned");
+  if (!step->lens_dev || !aligned(step->lens_dev, 4))
+    return fail(CM_EINVAL, "lens_dev is NULL or misaligned");
+  if (!step->table_dev || !aligned(step->table_dev, 4))
+    return fail(CM_EINVAL, "table_dev is NULL or misaligned");
+  if (step->table_width < 1 || step->table_width > (((int64_t)1 << 30) >> c.b_shift))
+    return fail(CM_EINVAL, "table_width must be in [1, 2^30 / block], got " +
+                               std::to_string(step->table_width));
+  if (step->n_rows == 0) return CM_OK;
+  if ((st = check_strides("q_dev", step->q_dev, esize, {step->q_row_stride, step->q_head_stride})) !=
+      CM_OK)
+    return st;
+  if ((st = check_strides("out_dev", step->out_dev, esize,
+                          {step->out_row_stride, step->out_head_stride})) != CM_OK)
+    return st;
+  if (step->lse_dev && !aligned(step->lse_dev, 4)) return fail(CM_EINVAL, "lse_dev is misaligned");
+  const cm::QAttentionPlan plan = qattention_plan(c, step);
+  if ((int64_t)plan.max_items * c.H > 0x7FFFFFFF)
+    return fail(CM_ESHAPE, "too many query rows for one call");
+  if ((st = check_ws(workspace, workspace_bytes, plan.bytes)) != CM_OK) return st;
+  cm::QAttention a;
+  const int64_t codes = c.slice_codes(), scales = c.slice_scales();
+  a.kc = c.codes + 2 * (int64_t)layer * codes;
+  a.vc = a.kc + codes;
+  a.ks = c.scales + 2 * (int64_t)layer * scales;
+  a.vs = a.ks + scales;
+  a.pages = c.pages;
+  a.H = c.H;
+  a.G = step->q_heads / c.H;
+  a.b_shift = c.b_shift;
+  a.n = step->n;
+  a.q = step->q_dev;
+  a.q_row = step->q_row_stride;
+  a.q_head = step->q_head_stride;
+  a.out = step->out_dev;
+  a.out_row = step->out_row_stride;
+  a.out_head = step->out_head_stride;
+  a.lse = step->lse_dev;
+  a.rows = step->rows_dev;
+  a.lens = step->lens_dev;
+  a.table = step->table_dev;
+  a.width = step->table_width;
+  a.n_rows = step->n_rows;
+  a.max_rows = step->max_rows;
+  a.window = step->window;
+  a.scale_log2 = step->scale * 1.4426950408889634f;
+  a.items = plan.items;
+  a.max_items = plan.max_items;
+  a.part = static_cast<float*>(workspace);
+  hipError_t e = cm::launch_qcache_attention(a, c.d, step->dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_attention");
 }
 
 int32_t cm_timing_enable(int32_t on) {

@@ -322,6 +322,10 @@ enum KernelId {
   K_RENDER_HASH,
   K_PAGED,
   K_PAGED_HASH_RENDER,
+  K_QCACHE_TABLES,
+  K_QCACHE_WRITE,
+  K_QCACHE_ATTENTION,
+  K_QCACHE_JOIN,
   K_COUNT
 };
 

@@ -1,0 +1,67 @@
+// Internal interface of the 8-bit paged cache (qcache_*.hip) and the layout of its
+// pages: codes [L][2][P][H][B][d], one OCP e4m3 number a byte, and scales [L][2][P][H].
+#pragma once
+
+#include "internal.h"
+
+namespace cm {
+
+struct QCacheDesc {
+  int32_t L, H, d, b_shift;  // B = 1 << b_shift
+  int64_t pages;
+  uint8_t* codes;
+  float* scales;
+  int64_t slice_codes() const { return ((pages * H) << b_shift) * d; }  // of one (layer, K/V)
+  int64_t slice_scales() const { return pages * H; }
+};
+
+// Rows of K or V of a step (cm_qrows), strides in bytes.
+struct QRows {
+  const uint8_t* data;
+  int64_t layer, token, head;
+};
+
+// What the attention kernels read and write (strides in elements).
+struct QAttention {
+  const uint8_t* kc;  // the layer's codes and scales
+  const uint8_t* vc;
+  const float* ks;
+  const float* vs;
+  int64_t pages;
+  int32_t H, G, b_shift, n;
+  const void* q;
+  int64_t q_row, q_head;
+  void* out;
+  int64_t out_row, out_head;
+  float* lse;
+  const int32_t* rows;
+  const int32_t* lens;
+  const int32_t* table;
+  int64_t width;
+  int64_t n_rows;
+  int32_t max_rows, window;
+  float scale_log2;   // softmax scale * log2(e)
+  int32_t items;      // work items that the lengths are cut into, for each KV head
+  int32_t max_items;  // bound of what that comes to
+  float* part;        // partial results [H][max_items][16][2 + d]
+};
+
+hipError_t launch_qcache_tables(int64_t pages, int32_t b_shift, int32_t n, const int32_t* held,
+                                const int32_t* fresh, const int32_t* free_pages, int64_t n_free,
+                                int32_t* table, int64_t width, int64_t n_tokens, int64_t* slots,
+                                int32_t* rows, int32_t* lens, int64_t* info, hipStream_t stream);
+hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t n_layers,
+                               int32_t dtype, const QRows& k, const QRows& v, int64_t n_tokens,
+                               const int64_t* slots, hipStream_t stream);
+
+// Work items of an attention call: the split that fills the GPU and the bound that
+// sizes its grid and its workspace, from what the host knows.
+struct QAttentionPlan {
+  int32_t items, max_items;
+  size_t bytes;
+};
+QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows);
+hipError_t launch_qcache_attention(const QAttention& a, int32_t d, int32_t dtype,
+                                   hipStream_t stream);
+
+}  // namespace cm

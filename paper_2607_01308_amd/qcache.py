@@ -1,0 +1,241 @@
+"""Serving a merged cache from 8-bit pages: the binding of cm_qcache_tables,
+cm_qcache_write and cm_qcache_attention (include/cmerge.h), and ServingCache, which
+strings them together for a set of requests.
+
+A cache holds, for each layer and K/V, pages of B tokens of every head: codes
+[L, 2, P, H, B, d] in float8_e4m3fn and scales [L, 2, P, H] in float32, one scale for a
+page and a head; a stored value is code * scale. Every call enqueues its work on one
+stream (the `stream` argument, else the current one), marks the tensors it was given as
+in use there and does not wait: lengths, tables and slots stay on the device."""
+
+from __future__ import annotations
+
+import ctypes
+from dataclasses import dataclass
+from typing import Dict, Optional, Sequence
+
+import torch
+
+from . import _cabi as C
+from .binding import _DTYPES
+
+CODES = torch.float8_e4m3fn
+
+
+class QCache:
+    """An 8-bit paged cache over tensors of the caller: codes [L, 2, P, H, B, d]
+    (float8_e4m3fn or uint8) and scales [L, 2, P, H] (float32), both contiguous and on
+    one GPU."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor):
+        if codes.dim() != 6 or codes.shape[1] != 2 or not codes.is_contiguous():
+            raise ValueError("codes must be a contiguous [L, 2, P, H, B, d] tensor")
+        if codes.dtype is not CODES and codes.dtype is not torch.uint8:
+            raise TypeError(f"codes must be float8_e4m3fn or uint8, got {codes.dtype}")
+        if scales.dtype is not torch.float32:
+            raise TypeError(f"scales must be float32, got {scales.dtype}")
+        if scales.shape != codes.shape[:4] or not scales.is_contiguous():
+            raise ValueError(f"scales must be a contiguous {list(codes.shape[:4])} tensor")
+        if not codes.is_cuda or scales.device != codes.device:
+            raise ValueError("codes and scales must live on one GPU")
+        self.codes, self.scales = codes, scales
+        self.device = codes.device
+        self.L, _, self.P, self.H, self.B, self.d = codes.shape
+        self.struct = C.CmQcache(self.L, self.H, self.d, self.B, self.P, codes.data_ptr(),
+                                 scales.data_ptr())
+
+    @classmethod
+    def empty(cls, L: int, H: int, d: int, pages: int, block: int = 16,
+              device="cuda") -> "QCache":
+        """A cache of zeros."""
+        codes = torch.zeros((L, 2, pages, H, block, d), dtype=torch.uint8, device=device)
+        return cls(codes.view(CODES), torch.zeros((L, 2, pages, H), device=device))
+
+    def __repr__(self) -> str:
+        return (f"QCache(L={self.L}, H={self.H}, d={self.d}, pages={self.P}, block={self.B}, "
+                f"device={self.device})")
+
+
+def _use(stream, device, *tensors) -> ctypes.c_void_p:
+    """The stream a call enqueues on, with the tensors its kernels read and write
+    marked as in use there: their memory must not go to another tensor before that
+    work has finished, whichever stream they were allocated on."""
+    s = stream if stream is not None else torch.cuda.current_stream(device)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(s)
+    return s
+
+
+def _check(t: torch.Tensor, name: str, dtype, device, shape=None) -> torch.Tensor:
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}, got {t.device}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+@dataclass
+class QCacheStep:
+    """What cm_qcache_tables makes of a step, on the device: slots [tokens] int64, rows
+    [n + 1] and lens [n] int32, info [4] int64 (status, tokens, pages taken, longest
+    length)."""
+    slots: torch.Tensor
+    rows: torch.Tensor
+    lens: torch.Tensor
+    info: torch.Tensor
+
+    def check(self) -> "QCacheStep":
+        """Waits for the step and raises if it was refused (nothing was written then)."""
+        status, tokens, pages, longest = self.info.tolist()
+        if status != C.CM_OK:
+            raise C.CmError(status, "cm_qcache_tables",
+                            f"the step was refused: {tokens} new tokens, {pages} pages needed, "
+                            f"longest request {longest} tokens (a length is negative, the new "
+                            "tokens are not as many as given, a table row is too short or the "
+                            "free list is)")
+        return self
+
+
+def qcache_tables(pages: int, block: int, held: torch.Tensor, new: torch.Tensor,
+                  free: torch.Tensor, table: torch.Tensor, tokens: int,
+                  stream=None) -> QCacheStep:
+    """cm_qcache_tables: the table rows [n, width] (in place), slots, rows and lengths
+    of a step in which request r, holding held[r] tokens, brings new[r] more; free: the
+    page ids to take from, in order; tokens: the sum of new."""
+    dev = table.device
+    if table.dim() != 2:
+        raise ValueError("table must be [n, width]")
+    n, width = table.shape
+    i32 = torch.int32
+    _check(table, "table", i32, dev)
+    _check(held, "held", i32, dev, (n,))
+    _check(new, "new", i32, dev, (n,))
+    _check(free, "free", i32, dev)
+    s = stream if stream is not None else torch.cuda.current_stream(dev)
+    with torch.cuda.stream(s):
+        # slots and info, then rows and lens, in one buffer
+        buf = torch.empty(tokens + 4 + n + 1, dtype=torch.int64, device=dev)
+        small = buf[tokens + 4:].view(i32)
+        step = QCacheStep(buf[:tokens], small[:n + 1], small[n + 1:2 * n + 1],
+                          buf[tokens:tokens + 4])
+    _use(s, dev, held, new, free, table)
+    base = buf.data_ptr()
+    C.check(C.lib().cm_qcache_tables(
+        pages, block, n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
+        table.data_ptr(), width, tokens, base, base + 8 * (tokens + 4),
+        base + 8 * (tokens + 4) + 4 * (n + 1), base + 8 * tokens, s.cuda_stream),
+        "cm_qcache_tables")
+    return step
+
+
+def _rows(x: torch.Tensor, name: str, cache: QCache, tokens: int):
+    if x.dim() == 3:
+        x = x.unsqueeze(0)
+    if x.dim() != 4 or x.shape[1:] != (tokens, cache.H, cache.d):
+        raise ValueError(f"{name} must be [layers, {tokens}, {cache.H}, {cache.d}], got "
+                         f"{list(x.shape)}")
+    if x.device != cache.device:
+        raise ValueError(f"{name} must live on {cache.device}")
+    if x.stride(3) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return x, C.CmQrows(x.data_ptr(), x.stride(0), x.stride(1), x.stride(2))
+
+
+def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
+                 slots: torch.Tensor, stream=None) -> None:
+    """cm_qcache_write: rows k and v, [tokens, H, d] of one layer or [layers, tokens, H, d]
+    of the layers from `layer` on, into their slots. Strides are free but for the last
+    dimension, in multiples of 16 bytes."""
+    tokens = slots.numel()
+    _check(slots, "slots", torch.int64, cache.device)
+    kt, kr = _rows(k, "k", cache, tokens)
+    vt, vr = _rows(v, "v", cache, tokens)
+    if k.dtype not in _DTYPES or v.dtype is not k.dtype:
+        raise TypeError(f"k and v must both be bfloat16 or float32, got {k.dtype} and {v.dtype}")
+    if kt.shape[0] != vt.shape[0]:
+        raise ValueError("k and v must have the same layers")
+    s = _use(stream, cache.device, cache.codes, cache.scales, k, v, slots)
+    C.check(C.lib().cm_qcache_write(ctypes.byref(cache.struct), layer, kt.shape[0],
+                                    _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens,
+                                    slots.data_ptr(), s.cuda_stream), "cm_qcache_write")
+
+
+_WS: Dict[tuple, torch.Tensor] = {}
+
+
+def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
+    """Scratch of the calls enqueued on a stream, cached for (device, stream) and
+    allocated there, so calls on two streams never share it."""
+    need = ctypes.c_size_t(0)
+    C.check(C.lib().cm_qcache_attention_size(ctypes.byref(cache.struct), ctypes.byref(step),
+                                             ctypes.byref(need)), "cm_qcache_attention_size")
+    key = (cache.device, s.cuda_stream)
+    ws = _WS.get(key)
+    if ws is None or ws.numel() < need.value:
+        with torch.cuda.stream(s):
+            ws = torch.empty(max(need.value, 256), dtype=torch.uint8, device=cache.device)
+        _WS[key] = ws
+    return ws
+
+
+def release_qcache_workspace() -> None:
+    _WS.clear()
+
+
+def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Tensor,
+                     lens: torch.Tensor, rows: Optional[torch.Tensor] = None,
+                     max_rows: Optional[int] = None, scale: Optional[float] = None,
+                     window: int = 0, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, stream=None):
+    """cm_qcache_attention: queries q [rows, q_heads, d] over one layer of the cache;
+    returns (out, lse). table [n, width], lens [n]: each request's pages and tokens, the
+    step's own included; rows [n + 1]: where each request's query rows begin (None: one
+    row for each request); max_rows: the most rows of a request (default: all of them,
+    or 1 without rows); scale: of the scores (default d ** -0.5); window: positions
+    that a query sees, itself included (0: all up to its own). out: q's shape and type;
+    lse [rows, q_heads] float32 (made if not given)."""
+    dev = cache.device
+    if q.dim() != 3 or q.shape[2] != cache.d:
+        raise ValueError(f"q must be [rows, q_heads, {cache.d}], got {list(q.shape)}")
+    if q.dtype not in _DTYPES:
+        raise TypeError(f"unsupported dtype {q.dtype} (bfloat16 or float32)")
+    if q.device != dev:
+        raise ValueError(f"q must live on {dev}")
+    n_rows, q_heads, d = q.shape
+    if q.stride(2) != 1:
+        raise ValueError("the last dimension of q must be contiguous")
+    if table.dim() != 2:
+        raise ValueError("table must be [n, width]")
+    n, width = table.shape
+    _check(table, "table", torch.int32, dev)
+    _check(lens, "lens", torch.int32, dev, (n,))
+    if rows is not None:
+        _check(rows, "rows", torch.int32, dev, (n + 1,))
+    if max_rows is None:
+        max_rows = 1 if rows is None else n_rows
+    s = stream if stream is not None else torch.cuda.current_stream(dev)
+    if out is None or lse is None:
+        with torch.cuda.stream(s):
+            if out is None:
+                out = torch.empty((n_rows, q_heads, d), dtype=q.dtype, device=dev)
+            if lse is None:
+                lse = torch.empty((n_rows, q_heads), dtype=torch.float32, device=dev)
+    if out.shape != q.shape or out.dtype is not q.dtype or out.device != dev or out.stride(2) != 1:
+        raise ValueError("out must have q's shape, type and device and a contiguous last dimension")
+    _check(lse, "lse", torch.float32, dev, (n_rows, q_heads))
+    step = C.CmQattention(
+        n, q_heads, _DTYPES[q.dtype], window, n_rows, max_rows,
+        d ** -0.5 if scale is None else scale, q.data_ptr(), q.stride(0), q.stride(1),
+        out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
+        None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
+    ws = _workspace(cache, step, s)
+    _use(s, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
+    C.check(C.lib().cm_qcache_attention(ctypes.byref(cache.struct), layer, ctypes.byref(step),
+                                        ws.data_ptr(), ws.numel(), s.cuda_stream),
+            "cm_qcache_attention")
+    return out, lse
