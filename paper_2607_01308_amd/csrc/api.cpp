@@ -1256,11 +1256,15 @@ int32_t check_qattention_shape(const cm::QCacheDesc& c, const cm_qattention* s) 
   if (s->n_rows < 0 || s->n_rows > 0x7FFFFFFF / s->q_heads)
     return fail(CM_EINVAL, "n_rows must be in [0, 2^31 / q_heads), got " + std::to_string(s->n_rows));
   if (s->max_rows < 0) return fail(CM_EINVAL, "max_rows must be >= 0");
+  if (s->table_width < 1 || s->table_width > (((int64_t)1 << 30) >> c.b_shift))
+    return fail(CM_EINVAL, "table_width must be in [1, 2^30 / block], got " +
+                               std::to_string(s->table_width));
   return CM_OK;
 }
 
 cm::QAttentionPlan qattention_plan(const cm::QCacheDesc& c, const cm_qattention* s) {
-  return cm::plan_qcache_attention(c.H, c.d, s->q_heads / c.H, s->n, s->n_rows);
+  return cm::plan_qcache_attention(c.H, c.d, s->q_heads / c.H, s->n, s->n_rows, s->max_rows,
+                                   s->table_width << c.b_shift);
 }
 
 }  // namespace
@@ -1363,9 +1367,6 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
     return fail(CM_EINVAL, "lens_dev is NULL or misaligned");
   if (!step->table_dev || !aligned(step->table_dev, 4))
     return fail(CM_EINVAL, "table_dev is NULL or misaligned");
-  if (step->table_width < 1 || step->table_width > (((int64_t)1 << 30) >> c.b_shift))
-    return fail(CM_EINVAL, "table_width must be in [1, 2^30 / block], got " +
-                               std::to_string(step->table_width));
   if (step->n_rows == 0) return CM_OK;
   if ((st = check_strides("q_dev", step->q_dev, esize, {step->q_row_stride, step->q_head_stride})) !=
       CM_OK)
@@ -1375,7 +1376,8 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
     return st;
   if (step->lse_dev && !aligned(step->lse_dev, 4)) return fail(CM_EINVAL, "lse_dev is misaligned");
   const cm::QAttentionPlan plan = qattention_plan(c, step);
-  if ((int64_t)plan.max_items * c.H > 0x7FFFFFFF)
+  if (((int64_t)plan.few_max + 8) * c.H > 0x7FFFFFFF ||
+      ((int64_t)plan.many_max + 8) * c.H > 0x7FFFFFFF)
     return fail(CM_ESHAPE, "too many query rows for one call");
   if ((st = check_ws(workspace, workspace_bytes, plan.bytes)) != CM_OK) return st;
   cm::QAttention a;
@@ -1403,10 +1405,19 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
   a.n_rows = step->n_rows;
   a.max_rows = step->max_rows;
   a.window = step->window;
-  a.scale_log2 = step->scale * 1.4426950408889634f;
-  a.items = plan.items;
-  a.max_items = plan.max_items;
-  a.part = static_cast<float*>(workspace);
+  a.scale_log2 = std::fabs(step->scale) * 1.4426950408889634f;
+  a.negate = step->scale < 0.f;
+  a.few_unit = plan.few_unit;
+  a.few_items = plan.few_items;
+  a.few_max = plan.few_max;
+  a.many_items = plan.many_items;
+  a.many_max = plan.many_max;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  a.few_part = reinterpret_cast<float*>(ws + plan.few_at);
+  a.many_part = reinterpret_cast<float*>(ws + plan.many_at);
+  a.few_count = reinterpret_cast<int32_t*>(ws);
+  a.many_count = a.few_count + 2 * (int64_t)plan.few_max * c.H;
+  a.split = plan.split;
   hipError_t e = cm::launch_qcache_attention(a, c.d, step->dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_attention");
 }

@@ -40,10 +40,18 @@ struct QAttention {
   int64_t width;
   int64_t n_rows;
   int32_t max_rows, window;
-  float scale_log2;   // softmax scale * log2(e)
-  int32_t items;      // work items that the lengths are cut into, for each KV head
-  int32_t max_items;  // bound of what that comes to
-  float* part;        // partial results [H][max_items][16][2 + d]
+  float scale_log2;   // |softmax scale| * log2(e)
+  int32_t negate;     // the softmax scale is negative
+  // For requests of few query rows and of many: the spans (few) or items (many) that their
+  // contexts are cut into for each KV head, places of partial results for each KV head,
+  // where they are, [H][max], and their counters, [H][max][2].
+  int32_t few_items, few_max, many_items, many_max;
+  float* few_part;
+  float* many_part;
+  int32_t* few_count;
+  int32_t* many_count;
+  int32_t few_unit;   // tokens by which few rows' contexts are cut
+  int32_t split;      // 0: no request is cut
 };
 
 hipError_t launch_qcache_tables(int64_t pages, int32_t b_shift, int32_t n, const int32_t* held,
@@ -56,11 +64,14 @@ hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t
 
 // Work items of an attention call: the split that fills the GPU and the bound that
 // sizes its grid and its workspace, from what the host knows.
+constexpr int64_t kCounters = 1 << 17;  // at the start of the workspace
 struct QAttentionPlan {
-  int32_t items, max_items;
-  size_t bytes;
+  int32_t few_unit, few_items, few_max, many_items, many_max;
+  bool split;
+  size_t few_at, many_at, bytes;  // partial results in the workspace, its size
 };
-QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows);
+QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows,
+                                     int32_t max_rows, int64_t longest);
 hipError_t launch_qcache_attention(const QAttention& a, int32_t d, int32_t dtype,
                                    hipStream_t stream);
 

@@ -44,4 +44,10 @@ __device__ __forceinline__ uint32_t scale_bits(uint32_t amax) {
   return (uint32_t)(e + 127) << 23;
 }
 
+// 1 in each byte of a word of four codes that is NaN (0x7F, 0xFF): a byte of
+// (w & 0x7F) + 1 reaches 0x80 only there.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t w) {
+  return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+}
+
 }  // namespace cm

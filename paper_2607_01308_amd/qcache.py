@@ -178,7 +178,8 @@ def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
     ws = _WS.get(key)
     if ws is None or ws.numel() < need.value:
         with torch.cuda.stream(s):
-            ws = torch.empty(max(need.value, 256), dtype=torch.uint8, device=cache.device)
+            # zero at first: the calls count in it, and leave their counters at zero
+            ws = torch.zeros(max(need.value, 256), dtype=torch.uint8, device=cache.device)
         _WS[key] = ws
     return ws
 
