@@ -1264,7 +1264,7 @@ int32_t check_qattention_shape(const cm::QCacheDesc& c, const cm_qattention* s) 
 
 cm::QAttentionPlan qattention_plan(const cm::QCacheDesc& c, const cm_qattention* s) {
   return cm::plan_qcache_attention(c.H, c.d, s->q_heads / c.H, s->n, s->n_rows, s->max_rows,
-                                   s->table_width << c.b_shift);
+                                   s->table_width << c.b_shift, s->dtype);
 }
 
 }  // namespace

@@ -71,7 +71,7 @@ struct QAttentionPlan {
   size_t few_at, many_at, bytes;  // partial results in the workspace, its size
 };
 QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows,
-                                     int32_t max_rows, int64_t longest);
+                                     int32_t max_rows, int64_t longest, int32_t dtype);
 hipError_t launch_qcache_attention(const QAttention& a, int32_t d, int32_t dtype,
                                    hipStream_t stream);
 

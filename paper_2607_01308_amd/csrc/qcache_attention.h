@@ -14,6 +14,11 @@ constexpr int kManyRows = 128;  // and of the kernel for many
 // other, whole.
 __host__ __device__ __forceinline__ bool few_rows(int64_t rows) { return rows <= kFewRows; }
 
+// Waves that share their rows in the kernel for many (qcache_prompt.hip): a wave's registers
+// hold its queries' terms, d * terms / 4 of them, and its columns of the output, d / 2; beyond
+// 96 two waves share.
+constexpr int many_halves(int d, int terms) { return d * (terms + 1) > 256 ? 2 : 1; }
+
 struct Item {
   int32_t r, tile, split, splits;  // request, row tile, range of its context, how many
   int32_t row0, count, len;        // the request's first row, rows, tokens
@@ -74,7 +79,7 @@ __device__ __forceinline__ int row_tiles(const QAttention& a, int count) {
 
 // What the workgroup shares while it looks for its item.
 struct FindShared {
-  float cost[8];
+  float cost[8], tiles[8];
   int items[8];
   Item it;
 };
@@ -90,7 +95,7 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int it
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (a.n + THREADS - 1) / THREADS;   // requests of a thread
   int row0[kPer], count[kPer], len[kPer], tiles[kPer], begin[kPer], units[kPer];
-  float cost = 0.f;
+  float cost = 0.f, all = 0.f;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int r = (int)threadIdx.x * per + k;
@@ -101,17 +106,28 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int it
       begin[k] = visible_begin(a, count[k], len[k]);
       units[k] = (len[k] - begin[k] + kUnit - 1) / kUnit;
       cost += (float)tiles[k] * (float)units[k];
+      all += (float)tiles[k];
     }
   }
   cost = wave_scan(cost);
+  all = wave_scan(all);
   if (threadIdx.x == 0) lds.it.any = 0;
-  if (lane == 63) lds.cost[wave] = cost;
+  if (lane == 63) {
+    lds.cost[wave] = cost;
+    lds.tiles[wave] = all;
+  }
   __syncthreads();
-  cost = 0.f;
+  cost = all = 0.f;
 #pragma unroll
-  for (int w = 0; w < THREADS / 64; ++w) cost += lds.cost[w];
-  // (a little more than the quotient: rounded sums must not make more items than the grid has)
-  const float want = cost / (float)items * 1.0001f;
+  for (int w = 0; w < THREADS / 64; ++w) {
+    cost += lds.cost[w];
+    all += lds.tiles[w];
+  }
+  // Each tile's ranges round up by about half a range, so that many fewer make `items` of them
+  // in all. (And a little more than the quotient: rounded sums must not make more items than
+  // the grid has.)
+  const float aim = fmaxf((float)items - 0.6f * all, 0.25f * (float)items);
+  const float want = cost / aim * 1.0001f;
   const int chunk = !a.split || want > 1e9f ? 1 << 30 : want > 1.f ? (int)want + 1 : 1;
   int splits[kPer], mine = 0;
 #pragma unroll
@@ -354,48 +370,65 @@ struct Joined {
   }
 };
 
-constexpr int kJoin = 16;   // partial results joined at a time
-
 // Joins `count` partial results, in the places slot(0), slot(1), ..: into the output (`whole`)
-// or, as the result of a group, into the first of them. In order, by all threads.
+// or, as the result of a group, into the first of them. In order, by all threads, each
+// several quads of columns at a time where there are few results to load for each.
+template <int ROWS, int D, int ES, int THREADS, int BATCH, int QUADS, class Slot>
+__device__ __forceinline__ void join_some(const QAttention& a, const Item& it, int h, int count,
+                                          int level, bool whole, Slot slot) {
+  constexpr int kQuads = D / 4;
+  const int left = it.count * a.G - it.tile * ROWS;
+  const int total = (left < ROWS ? left : ROWS) * kQuads;
+  const Part<ROWS, D> p0 = part_of<ROWS, D>(a, h, slot(0));
+  for (int x0 = threadIdx.x; x0 < total; x0 += THREADS * QUADS) {
+    Joined sum[QUADS];
+    for (int s = 0; s < count; s += BATCH) {
+      f32x4 o[QUADS][BATCH];
+      float m[QUADS][BATCH], l[QUADS][BATCH];
+#pragma unroll
+      for (int k = 0; k < BATCH; ++k) {
+        const Part<ROWS, D> p = part_of<ROWS, D>(a, h, slot(s + k < count ? s + k : s));
+#pragma unroll
+        for (int u = 0; u < QUADS; ++u) {
+          const int x = x0 + u * THREADS < total ? x0 + u * THREADS : x0;
+          o[u][k] = p.quad(x / kQuads, x % kQuads);
+          p.stat(level, x / kQuads, m[u][k], l[u][k]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < QUADS; ++u) {
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+          const bool there = s + k < count;      // (what is not there weighs nothing)
+          o[u][k] = there ? o[u][k] : f32x4{0.f, 0.f, 0.f, 0.f};
+          m[u][k] = there ? m[u][k] : kNone;
+          l[u][k] = there ? l[u][k] : 0.f;
+        }
+        sum[u].add(o[u], m[u], l[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < QUADS; ++u) {
+      const int x = x0 + u * THREADS;
+      if (x >= total) break;
+      const int row = x / kQuads, quad = x % kQuads;
+      if (whole) {
+        const RowPlace place = row_place(a, it, h, it.tile * ROWS + row);
+        put_quad<ES>(a, place, 4 * quad, sum[u].o, sum[u].l);
+        if (quad == 0) put_lse(a, place, sum[u].m == kNone ? 0.f : sum[u].m, sum[u].l);
+      } else {
+        p0.put_quad(row, quad, sum[u].o);        // (read by this thread alone)
+        if (quad == 0) p0.put_stat(1, row, sum[u].m, sum[u].l);
+      }
+    }
+  }
+}
+constexpr int kJoin = 16;   // partial results joined at a time
 template <int ROWS, int D, int ES, int THREADS, class Slot>
 __device__ __forceinline__ void join_parts(const QAttention& a, const Item& it, int h, int count,
                                            int level, bool whole, Slot slot) {
-  constexpr int kQuads = D / 4;
-  const int left = it.count * a.G - it.tile * ROWS;
-  const int rows = left < ROWS ? left : ROWS;
-  const Part<ROWS, D> p0 = part_of<ROWS, D>(a, h, slot(0));
-  for (int x = threadIdx.x; x < rows * kQuads; x += THREADS) {
-    const int row = x / kQuads, quad = x % kQuads;
-    Joined sum;
-    for (int s = 0; s < count; s += kJoin) {
-      f32x4 o[kJoin];
-      float m[kJoin], l[kJoin];
-#pragma unroll
-      for (int k = 0; k < kJoin; ++k) {
-        const bool there = s + k < count;        // (what is not there weighs nothing)
-        const Part<ROWS, D> p = part_of<ROWS, D>(a, h, slot(there ? s + k : s));
-        o[k] = p.quad(row, quad);
-        p.stat(level, row, m[k], l[k]);
-      }
-#pragma unroll
-      for (int k = 0; k < kJoin; ++k) {
-        const bool there = s + k < count;
-        o[k] = there ? o[k] : f32x4{0.f, 0.f, 0.f, 0.f};
-        m[k] = there ? m[k] : kNone;
-        l[k] = there ? l[k] : 0.f;
-      }
-      sum.add(o, m, l);
-    }
-    if (whole) {
-      const RowPlace place = row_place(a, it, h, it.tile * ROWS + row);
-      put_quad<ES>(a, place, 4 * quad, sum.o, sum.l);
-      if (quad == 0) put_lse(a, place, sum.m == kNone ? 0.f : sum.m, sum.l);
-    } else {
-      p0.put_quad(row, quad, sum.o);             // (read by this thread alone)
-      if (quad == 0) p0.put_stat(1, row, sum.m, sum.l);
-    }
-  }
+  if (count <= 4) join_some<ROWS, D, ES, THREADS, 4, 4>(a, it, h, count, level, whole, slot);
+  else join_some<ROWS, D, ES, THREADS, 8, 2>(a, it, h, count, level, whole, slot);
 }
 
 // Whether this workgroup is the last of `count` to come to a counter, which the last one

@@ -237,8 +237,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
       float best = e[0];
 #pragma unroll
       for (int k = 1; k < 8; ++k) best = fmaxf(best, e[k]);
-      best = fmaxf(best, __shfl_xor(best, 16));
-      best = fmaxf(best, __shfl_xor(best, 32));
+      best = lane_max<32>(lane_max<16>(best));
       const float m = fmaxf(top, best);
       const float low = m == kNone ? 0.f : m;
       if (__any(m != top)) {
@@ -286,8 +285,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
   }
 
   // the waves' results as one, half of the waves to the other half at a time
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  l = lane_sum<32>(lane_sum<16>(l));
 #pragma unroll
   for (int half = WAVES / 2; half >= 1; half >>= 1) {
     if (wave >= half && wave < 2 * half) {
@@ -399,34 +397,35 @@ __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
     it.r = r;
     it.begin = visible_begin(a, it.count, it.len);
   };
-  if (!a.split) {
-    for (int r = w; r < a.n; r += a.few_items) {
-      if (lds.pos[r] == lds.pos[r + 1]) continue;
+  // (with spans: request after request until the span's end; without: every few_items-th)
+  int r = a.split ? __builtin_amdgcn_readfirstlane(lds.first) : w;
+  while (a.split ? u < stop : r < a.n) {
+    const int from = __builtin_amdgcn_readfirstlane(lds.pos[r]);
+    const int to = __builtin_amdgcn_readfirstlane(lds.pos[r + 1]);
+    if (from != to) {
       look(r);
       it.splits = 1;
       it.chunk = it.len - it.begin;
-      few_rows_segment<TERMS, D, WAVES>(a, it, h, 0, lds);
+      int part = 0, first = 0;
+      if (a.split) {
+        const int upto_u = to < stop ? to : stop;
+        it.begin += (u - from) * a.few_unit;
+        it.chunk = (upto_u - u) * a.few_unit;
+        u = upto_u;
+        // the spans that hold some of it
+        first = from / span;
+        part = w - first;
+        it.splits = (to - 1) / span - first + 1;
+      }
+      // (in the first of them another request may come before it)
+      const auto slot = [&](int i) {
+        return i == 0 ? 2 * first + (from > first * span ? 1 : 0) : 2 * (first + i);
+      };
+      few_rows_segment<TERMS, D, WAVES>(a, it, h, slot(part), lds);
+      if (it.splits > 1)
+        finish_split<kFewRows, D, ES, kThreads>(a, it, h, part, it.splits, &lds.flag, slot);
     }
-    return;
-  }
-  for (int r = __builtin_amdgcn_readfirstlane(lds.first); u < stop; ++r) {
-    const int from = __builtin_amdgcn_readfirstlane(lds.pos[r]);
-    const int to = __builtin_amdgcn_readfirstlane(lds.pos[r + 1]);
-    if (from == to) continue;
-    const int upto_u = to < stop ? to : stop;
-    look(r);
-    it.begin += (u - from) * a.few_unit;
-    it.chunk = (upto_u - u) * a.few_unit;
-    // the spans that hold some of it; the first may hold more before it
-    const int first = from / span, last = (to - 1) / span;
-    it.splits = last - first + 1;
-    const auto slot = [&](int i) {
-      return i == 0 ? 2 * first + (from > first * span ? 1 : 0) : 2 * (first + i);
-    };
-    few_rows_segment<TERMS, D, WAVES>(a, it, h, slot(w - first), lds);
-    if (it.splits > 1)
-      finish_split<kFewRows, D, ES, kThreads>(a, it, h, w - first, it.splits, &lds.flag, slot);
-    u = upto_u;
+    r += a.split ? 1 : a.few_items;
   }
 }
 

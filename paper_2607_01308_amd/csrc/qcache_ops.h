@@ -36,6 +36,34 @@ __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d)
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
+// max and sum of a value and that of the lane 16 or 32 away (exchanged within the
+// vector registers, not through the LDS, whose queue they would wait for).
+template <int BY>
+__device__ __forceinline__ void lane_pair(float x, float& a, float& b) {
+  const uint32_t u = __float_as_uint(x);
+  if constexpr (BY == 32) {
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    a = __uint_as_float(r[0]);
+    b = __uint_as_float(r[1]);
+  } else {
+    const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    a = __uint_as_float(r[0]);
+    b = __uint_as_float(r[1]);
+  }
+}
+template <int BY>
+__device__ __forceinline__ float lane_max(float x) {
+  float a, b;
+  lane_pair<BY>(x, a, b);
+  return fmaxf(a, b);
+}
+template <int BY>
+__device__ __forceinline__ float lane_sum(float x) {
+  float a, b;
+  lane_pair<BY>(x, a, b);
+  return a + b;
+}
+
 // Bits of the least 2^e, e >= -120, with amax <= 448 * 2^e (448 = 1.75 * 2^8), from
 // the bits of a finite amax >= 0.
 __device__ __forceinline__ uint32_t scale_bits(uint32_t amax) {

@@ -5,9 +5,8 @@
 // the other way round: a workgroup takes 128 query rows (a request's rows times the
 // group) of one KV head, each of its four waves 32 of them, and walks the context in
 // tiles of TOK tokens. A tile's codes are turned into bf16 once for all 128 rows, by 2^e of
-// their page's scale on the way (the conversion takes the power of two at no cost; scales
-// that are no powers of two leave a factor in [1, 2) for the scores and the
-// probabilities), and staged in the LDS: K row-major, V transposed. Both products are
+// their page's scale on the way (the conversion takes the power of two at no cost; what is left
+// of a scale that is none goes into the exponents), and staged in the LDS: K row-major, V transposed. Both products are
 // computed transposed by 32x32x16 matrix instructions, S^T = K Q^T and out^T = V^T P^T, so that a
 // lane holds of S^T exactly the probabilities that it has to supply of P^T; V's columns
 // are laid out in that order of the tokens: element e of 16-byte chunk 2 s + k of a row is
@@ -35,17 +34,19 @@ __device__ __forceinline__ uint32_t scaled_bf16(uint32_t w, float pow) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow, HI));
 }
 
-// Bytes of the K and V tiles, and a chunk's place in them.
+// Bytes of the K and V tiles, and a chunk's place in them. The rows' numbers are combined with
+// the chunks' by exclusive or, so the places of a lane's chunks are its first one's with
+// some bits of their numbers turned.
 template <int D, int TOK>
 struct Tile {
   static constexpr int kBytes = D * TOK * 2;
   // K: row = token, D / 8 chunks
-  static __device__ __forceinline__ int k_at(int tok, int chunk) {
+  static __device__ __forceinline__ uint32_t k_at(int tok, int chunk) {
     const int x = D == 64 ? (tok >> 1) & 7 : tok & 15;
     return tok * D * 2 + ((chunk ^ x) << 4);
   }
   // V: row = column of V, TOK / 8 chunks
-  static __device__ __forceinline__ int v_at(int col, int chunk) {
+  static __device__ __forceinline__ uint32_t v_at(int col, int chunk) {
     const int x = TOK == 32 ? (col >> 2) & 3 : ((col >> 1) & 7) ^ ((col >> 4) & 1);
     return col * TOK * 2 + ((chunk ^ x) << 4);
   }
@@ -66,7 +67,6 @@ struct ManyShared {
   uint8_t v[2][D * TOK * 2];
   // halves of scores that waves exchange
   f32x4 half[HALVES == 2 ? kRowWaves * HALVES * (TOK / 32) * 4 * 64 : 1];
-  int odd[64 / (TOK / 16)];                      // a value that is not finite among a tile's V
   FindShared find;
   int flag;
 };
@@ -127,11 +127,14 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const int64_t page_codes = ((int64_t)a.H << a.b_shift) * D;
   const int64_t head_codes = ((int64_t)h << a.b_shift) * D;
 
-  // 64 groups at a time: their pages and scales, one lane each
+  // 64 groups at a time: their pages and scales, one lane each. A scale is a power of two,
+  // which the conversion to bf16 takes, times a rest in [1, 2), which the scores' factor
+  // takes for K and the exponent of the probabilities for V: 2^(x - ref + log2 rest) goes into
+  // the product, and its sum over a group divided by the rest into l.
   int32_t my_page = 0;
   float my_ks = 0.f, my_vs = 0.f;                // the powers of two
-  float my_kf = 1.f, my_vf = 1.f;                // what is left of the scales
-  uint64_t absent = 0, uneven = 0;
+  float my_kf = 0.f, my_vl = 0.f, my_vi = 1.f;   // scores' factor; log2 and inverse of V's rest
+  uint64_t absent = 0;
   const auto look_up = [&](int t0) {
     const int my_t = t0 + lane * 16;
     bool there = false;
@@ -144,69 +147,72 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       ks = a.ks[(int64_t)my_page * a.H + h];
       vs = a.vs[(int64_t)my_page * a.H + h];
     }
-    const auto split = [](float s, float& pow, float& rest) {
+    const auto split = [](float s, float& pow) {
       const uint32_t e = __float_as_uint(s) & 0x7F800000u;
       pow = __uint_as_float(e);
-      // (an exponent field of 0 stands for 2^-127 in the conversion)
-      rest = e == 0 ? s * 0x1p127f : __uint_as_float((__float_as_uint(s) & 0x807FFFFFu) | 0x3F800000u);
+      // (an exponent field of 0 stands for 2^-127 in the conversion; a scale of 0 is that)
+      if (e == 0) return s == 0.f ? 1.f : fabsf(s) * 0x1p127f;
+      return __uint_as_float((__float_as_uint(s) & 0x7FFFFFu) | 0x3F800000u);
     };
-    split(ks, my_ks, my_kf);
-    split(vs, my_vs, my_vf);
+    my_kf = split(ks, my_ks) * a.scale_log2;
+    const float rest = split(vs, my_vs);
+    my_vl = __builtin_amdgcn_logf(rest);
+    my_vi = 1.f / rest;
     absent = ~__ballot(there);
-    uneven = __ballot(my_kf != 1.f || my_vf != 1.f);
   };
   // The wave's share of a tile: group `wave % kGroups`, columns from wave / kGroups * COLS.
-  const int my_group = wave % kGroups, col0 = wave / kGroups * COLS;
+  const int my_group = __builtin_amdgcn_readfirstlane(wave % kGroups);
+  const int col0 = __builtin_amdgcn_readfirstlane(wave / kGroups * COLS);
+  // K: lane = (token lane / 4, quarter of the columns). V: lane = (tokens 4 g + i and 8 + 4 g + i,
+  // four columns) or, for 64 columns, (tokens 4 (lane / 16) + i, four columns).
+  const uint32_t k_load = (lane >> 2) * D + (lane & 3) * (COLS / 4) + col0;
+  const uint32_t v_load = (COLS == 128 ? 4 * g * D + 4 * n : 4 * (lane >> 4) * D + 4 * (lane & 15)) + col0;
   const auto load = [&](int tile, Codes<COLS>& x) {
     const int gi = (tile * kGroups + my_group) & 63;
     const int64_t page = __builtin_amdgcn_readlane(my_page, gi);
-    const int row = (begin + tile * TOK + my_group * 16) & (B - 1);
-    const int64_t base = page * page_codes + head_codes + (int64_t)row * D + col0;
-    // K: lane = (token lane / 4, quarter of the columns)
-    const uint8_t* kp = a.kc + base + (lane >> 2) * D + (lane & 3) * (COLS / 4);
+    const int row = __builtin_amdgcn_readfirstlane((begin + tile * TOK + my_group * 16) & (B - 1));
+    const int64_t base = page * page_codes + head_codes + (int64_t)row * D;
+    const uint8_t* kp = a.kc + base;
 #pragma unroll
-    for (int w = 0; w < COLS / 64; ++w) x.k[w] = *(global_ptr<u32x4>(kp) + w);
+    for (int w = 0; w < COLS / 64; ++w) x.k[w] = *global_ptr<u32x4>(kp + (k_load + 16 * w));
     const uint8_t* vp = a.vc + base;
-    if constexpr (COLS == 128) {
-      // V: lane = (tokens 4 g + i and 8 + 4 g + i, four columns)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        x.v[i] = *global_ptr<uint32_t>(vp + ((i & 3) + 4 * g + 8 * (i >> 2)) * D + 4 * n);
-    } else {
-      // V: lane = (tokens 4 (lane / 16) + i, four columns)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x.v[i] = *global_ptr<uint32_t>(vp + (4 * (lane >> 4) + i) * D + 4 * (lane & 15));
-    }
+    for (int i = 0; i < COLS / 16; ++i)
+      x.v[i] = *global_ptr<uint32_t>(vp + (v_load + ((i & 3) + 8 * (i >> 2)) * D));
+  };
+  // A lane's places in the LDS: what it reads of K and V, what it stages of them.
+  const uint32_t k_read = T::k_at(n, half * (DH / 8) + g);
+  const uint32_t v_read = T::v_at(half * DH + n, g);
+  const uint32_t k_write =
+      T::k_at(my_group * 16 + (lane >> 2), (col0 + (lane & 3) * (COLS / 4)) / 8);
+  const uint32_t v_write =
+      COLS == 128 ? T::v_at(col0 + 4 * n, 2 * my_group + g)
+                  : T::v_at(col0 + 4 * (lane & 15), 2 * my_group + ((lane >> 4) & 1)) +
+                        8 * (lane >> 5);
+  // (opaque: computed again for each tile, not kept for all of them in registers)
+  const auto fresh = [](uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
   };
   const auto stage = [&](int tile, const Codes<COLS>& x, int buf) {
     const int gi = (tile * kGroups + my_group) & 63;
     const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), gi));
     const float vs = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vs), gi));
-    {
-      const int t = my_group * 16 + (lane >> 2);
+    const uint32_t kw = fresh(k_write), vw = fresh(v_write);
 #pragma unroll
-      for (int w = 0; w < COLS / 64; ++w)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t lo = x.k[w][2 * half], hi2 = x.k[w][2 * half + 1];
-          const u32x4 o = {scaled_bf16<false>(lo, ks), scaled_bf16<true>(lo, ks),
-                           scaled_bf16<false>(hi2, ks), scaled_bf16<true>(hi2, ks)};
-          const int chunk = (col0 + (lane & 3) * (COLS / 4)) / 8 + 2 * w + half;
-          *reinterpret_cast<u32x4*>(&lds.k[buf][T::k_at(t, chunk)]) = o;
-        }
+    for (int w = 0; w < COLS / 32; ++w) {
+      const uint32_t lo = x.k[w >> 1][2 * (w & 1)], hi2 = x.k[w >> 1][2 * (w & 1) + 1];
+      const u32x4 o = {scaled_bf16<false>(lo, ks), scaled_bf16<true>(lo, ks),
+                       scaled_bf16<false>(hi2, ks), scaled_bf16<true>(hi2, ks)};
+      *reinterpret_cast<u32x4*>(&lds.k[buf][kw ^ (w << 4)]) = o;
     }
-    bool odd = false;
     constexpr int NV = COLS / 16;                // tokens of a lane
     uint32_t lo[NV], hi2[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      odd |= nan_codes(x.v[i]) != 0;
       lo[i] = scaled_bf16<false>(x.v[i], vs);
       hi2[i] = scaled_bf16<true>(x.v[i], vs);
     }
-    odd |= (__float_as_uint(vs) & 0x7F800000u) == 0x7F800000u;
-    if (odd) lds.odd[tile & (kPerLook - 1)] = 1;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const uint32_t sel = c & 1 ? 0x07060302u : 0x05040100u;
@@ -215,52 +221,54 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       for (int k = 0; k < NV / 2; ++k)
         o[k] = c < 2 ? __builtin_amdgcn_perm(lo[2 * k + 1], lo[2 * k], sel)
                      : __builtin_amdgcn_perm(hi2[2 * k + 1], hi2[2 * k], sel);
-      if constexpr (COLS == 128) {
-        *reinterpret_cast<u32x4*>(&lds.v[buf][T::v_at(col0 + 4 * n + c, 2 * my_group + g)]) =
-            u32x4{o[0], o[1], o[2], o[3]};
-      } else {
-        // tokens 4 quad + i: chunk 2 group + quad % 2, half quad / 2
-        const int quad = lane >> 4;
-        *reinterpret_cast<u32x2*>(
-            &lds.v[buf][T::v_at(col0 + 4 * (lane & 15) + c, 2 * my_group + (quad & 1)) +
-                      8 * (quad >> 1)]) = u32x2{o[0], o[1]};
-      }
+      // column 4 n + c: its row's number differs from that of c = 0 in c / 2 (TOK 64)
+      uint8_t* at = &lds.v[buf][(vw ^ (TOK == 64 ? (c >> 1) << 4 : 0)) + c * TOK * 2];
+      if constexpr (COLS == 128) *reinterpret_cast<u32x4*>(at) = u32x4{o[0], o[1], o[2], o[3]};
+      else *reinterpret_cast<u32x2*>(at) = u32x2{o[0], o[1]};
     }
   };
 
-  // The tile's scores, of this wave's half of d.
-  const auto scores = [&](f32x16 (&sc)[kTok32], int buf) {
+  // Operands come from the LDS four products ahead.
+  constexpr int kAhead = 4;
+  const auto k_operand = [&](uint32_t kr, int buf, int e) {  // product e = c * kTok32 + b of the scores
+    const int b = e % kTok32, c = e / kTok32;
+    return *reinterpret_cast<const u32x4*>(&lds.k[buf][(kr ^ (c << 5)) + b * 32 * D * 2]);
+  };
+  const auto v_operand = [&](uint32_t vr, int buf, int e) {  // product e = s * DH / 32 + j of the output
+    const int s = e / (DH / 32), j = e % (DH / 32);
+    return *reinterpret_cast<const u32x4*>(&lds.v[buf][(vr ^ (s << 5)) + j * 32 * TOK * 2]);
+  };
+  constexpr int kScoreOps = kTok32 * (DH / 16), kOutOps = kGroups * (DH / 32);
+  static_assert(kScoreOps >= kAhead && kOutOps >= kAhead, "");
+  // The tile's scores, of this wave's half of d; leaves the first operands of V in f.
+  const auto scores = [&](f32x16 (&sc)[kTok32], u32x4 (&f)[kAhead], int buf) {
+    const uint32_t kr = fresh(k_read), vr = fresh(v_read);
 #pragma unroll
     for (int b = 0; b < kTok32; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
 #pragma unroll
-    for (int c = 0; c < DH / 16; ++c) {
+    for (int e = 0; e < kAhead; ++e) f[e] = k_operand(kr, buf, e);
 #pragma unroll
-      for (int b = 0; b < kTok32; ++b) {
-        const bf16x8 k = __builtin_bit_cast(
-            bf16x8, *reinterpret_cast<const u32x4*>(
-                        &lds.k[buf][T::k_at(32 * b + n, half * (DH / 8) + 2 * c + g)]));
+    for (int e = 0; e < kScoreOps; ++e) {
+      const bf16x8 k = __builtin_bit_cast(bf16x8, f[e % kAhead]);
+      const int b = e % kTok32, c = e / kTok32;
 #pragma unroll
-        for (int w = TERMS - 1; w >= 0; --w)
-          sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c][w], sc[b], 0, 0, 0);
-      }
+      for (int w = TERMS - 1; w >= 0; --w)
+        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c][w], sc[b], 0, 0, 0);
+      f[e % kAhead] = e + kAhead < kScoreOps ? k_operand(kr, buf, e + kAhead)
+                                             : v_operand(vr, buf, e + kAhead - kScoreOps);
+
     }
   };
   // The rest of a tile; register i of sc[b] is token 32 b + 8 (i / 4) + 4 g + i % 4 of row n.
   // seen: every row sees every token of the tile.
-  const auto compute = [&](f32x16 (&sc)[kTok32], bool seen, int tile, int buf) {
+  const auto compute = [&](f32x16 (&sc)[kTok32], u32x4 (&f)[kAhead], bool seen, int tile, int buf) {
     const int t = begin + tile * TOK;
     const int g0 = (tile * kGroups) & 63;        // the tile's first group among those looked up
-    const bool plain = ((uneven >> g0) & ((1ull << kGroups) - 1)) == 0;
-    if (!plain) {
-#pragma unroll
-      for (int s = 0; s < kGroups; ++s) {
-        const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_kf), g0 + s));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sc[s >> 1][8 * (s & 1) + i] *= f;
-      }
-    }
+    const auto of_group = [&](float x, int s) {
+      return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), g0 + s));
+    };
     if (!seen) {
       const int lo = see_lo - t - 4 * g, hi = see_hi - t - 4 * g;
 #pragma unroll
@@ -272,13 +280,16 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
           sc[b][i] = tt >= lo && tt < hi && !gone ? sc[b][i] : kNone;
         }
     }
-    float best = sc[0][0];
+    float best = kNone;
 #pragma unroll
-    for (int b = 0; b < kTok32; ++b)
+    for (int s = 0; s < kGroups; ++s) {
+      float x = sc[s >> 1][8 * (s & 1)];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) best = fmaxf(best, sc[b][i]);
-    best = fmaxf(best, __shfl_xor(best, 32));
-    top = fmaxf(top, best * a.scale_log2);
+      for (int i = 1; i < 8; ++i) x = fmaxf(x, sc[s >> 1][8 * (s & 1) + i]);
+      best = fmaxf(best, x * of_group(my_kf, s));
+    }
+    best = lane_max<32>(best);
+    top = fmaxf(top, best);
     // acc and l stay relative to an earlier maximum while the new one is less than 2^8 times it
     if (__any(top > ref + 8.f)) {
       const float shrink = top == kNone ? 1.f : __builtin_amdgcn_exp2f(ref - top);
@@ -294,50 +305,45 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
     // weight may be more than 1/32 of a row's sum, then one (an error of 2^-8 of 2^-5)
     bool fine = TERMS == 3;
     if constexpr (TERMS == 1) {
-      const float whole = l + __shfl_xor(l, 32);
+      const float whole = lane_sum<32>(l);
       fine = __any(live && !(whole >= 32.f * __builtin_amdgcn_exp2f(top - low)));
     }
+    const uint32_t vr = fresh(v_read);
+    // out^T += V^T P^T, 16 tokens at a time: registers 8 (s % 2) .. of sc[s / 2]
+    const auto products = [&](int s) {
+      u32x4 w;
 #pragma unroll
-    for (int b = 0; b < kTok32; ++b)
+      for (int k = 0; k < 4; ++k)
+        w[k] = pair_bf16(sc[s >> 1][8 * (s & 1) + 2 * k], sc[s >> 1][8 * (s & 1) + 2 * k + 1]);
+      const bf16x8 pt = __builtin_bit_cast(bf16x8, w);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[b][i] = __builtin_amdgcn_exp2f(fmaf(sc[b][i], a.scale_log2, -low));
-        l += sc[b][i];
+      for (int j = 0; j < DH / 32; ++j) {
+        const int e = s * (DH / 32) + j;
+        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[e % kAhead]), pt,
+                                                         acc[j], 0, 0, 0);
+        if (e + kAhead < kOutOps) f[e % kAhead] = v_operand(vr, buf, e + kAhead);
       }
-    if (!plain) {
+    };
+    const auto exponents = [&](int s) {
+      const float kf = of_group(my_kf, s), off = of_group(my_vl, s) - low;
+      float sum = 0.f;
 #pragma unroll
-      for (int s = 0; s < kGroups; ++s) {
-        const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vf), g0 + s));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {            // (the scale may be NaN where nothing is seen)
-          const float x = sc[s >> 1][8 * (s & 1) + i];
-          sc[s >> 1][8 * (s & 1) + i] = x == 0.f ? 0.f : x * f;
-        }
+      for (int i = 0; i < 8; ++i) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(sc[s >> 1][8 * (s & 1) + i], kf, off));
+        sc[s >> 1][8 * (s & 1) + i] = x;
+        sum += x;
       }
+      l = fmaf(sum, of_group(my_vi, s), l);
+    };
+    exponents(0);
+#pragma unroll
+    for (int s = 0; s < kGroups; ++s) {
+      if (s + 1 < kGroups) exponents(s + 1);
+      products(s);
     }
-    // out^T += V^T P^T, one term of the probabilities after the other
-    for (int more = TERMS == 3 ? 2 : fine ? 1 : 0;; --more) {
-#pragma unroll
-      for (int s = 0; s < kGroups; ++s) {        // 16 tokens: registers 8 (s % 2) .. of sc[s / 2]
-        u32x4 w;
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          w[k] = pair_bf16(sc[s >> 1][8 * (s & 1) + 2 * k], sc[s >> 1][8 * (s & 1) + 2 * k + 1]);
-        const bf16x8 pt = __builtin_bit_cast(bf16x8, w);
-#pragma unroll
-        for (int j = 0; j < DH / 32; ++j) {
-          const u32x4 v = *reinterpret_cast<const u32x4*>(
-              &lds.v[buf][T::v_at(half * DH + 32 * j + n, 2 * s + g)]);
-          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), pt, acc[j],
-                                                           0, 0, 0);
-        }
-      }
-      if (more == 0) break;
-      // (what follows belongs to the next term alone: nothing of it, nor the loads of V,
-      // is to move before the branch)
-      asm volatile("" ::: "memory");
-#pragma unroll
-      for (int b = 0; b < kTok32; ++b) asm volatile("" : "+v"(sc[b]));
+
+    for (int more = TERMS == 3 ? 2 : fine ? 1 : 0; more > 0; --more) {
+      // what the terms so far have left of the probabilities
 #pragma unroll
       for (int b = 0; b < kTok32; ++b)
 #pragma unroll
@@ -346,14 +352,26 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
           sc[b][i] -= low_bf16(w);
           sc[b][i + 1] -= high_bf16(w);
         }
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) f[e] = v_operand(vr, buf, e);
+#pragma unroll
+      for (int s = 0; s < kGroups; ++s) products(s);
     }
   };
 
-  // Values of V that are not finite, in a tile that some row sees only in part: a product
-  // of their places with what each row sees finds the rows and columns that become NaN;
-  // then they are taken out of the tile, since 0 * NaN would reach the other rows. (Rare,
-  // and all waves come here together.)
+  // In a tile that some row sees only in part, values of V that are not finite: a product of
+  // their places with what each row sees finds the rows and columns that become NaN; then
+  // they are taken out of the tile, since 0 * NaN would reach the other rows. (All waves come
+  // here together.)
   const auto take_out = [&](int tile, int buf) {
+    int odd = 0;
+    for (int x = threadIdx.x; x < T::kBytes / 16; x += 64 * kWaves) {
+      const u32x4 v = *reinterpret_cast<const u32x4*>(&lds.v[buf][16 * x]);
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        odd |= (v[k] & 0x7F80u) == 0x7F80u || (v[k] & 0x7F800000u) == 0x7F800000u;
+    }
+    if (!__syncthreads_or(odd)) return;
     const int t = begin + tile * TOK;
     const int g0 = (tile * kGroups) & 63;
 #pragma unroll 1
@@ -398,61 +416,71 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
     __syncthreads();
   };
 
-  // Tiles: loaded two ahead, staged one ahead, one barrier each. Look-ups are for 64
-  // groups; a tile's groups never straddle two of them.
-  for (int base = 0; base < tiles; base += kPerLook) {
-    if (threadIdx.x < kPerLook) lds.odd[threadIdx.x] = 0;
-    look_up(begin + base * TOK);
-    const int stop = tiles - base < kPerLook ? tiles : base + kPerLook;
-    Codes<COLS> x;
-    load(base, x);
-    __syncthreads();
-    stage(base, x, base & 1);
-    if (base + 1 < stop) load(base + 1, x);
-    __syncthreads();
-    for (int i = base; i < stop; ++i) {
-      const int t = begin + i * TOK;
-      const uint64_t mask = ((1ull << kGroups) - 1) << ((i * kGroups) & 63);
-      const bool seen = t >= sight.all_lo && t + TOK <= sight.all_hi && (absent & mask) == 0;
-      if (!seen && lds.odd[i & (kPerLook - 1)] != 0) take_out(i, i & 1);
-      f32x16 sc[kTok32];
-      if constexpr (HALVES == 1) {
-        if (wave_live) {
-          scores(sc, i & 1);
-          compute(sc, seen, i, i & 1);
-        }
-      } else {
-        if (wave_live) scores(sc, i & 1);
-        const auto place = [&](int h2, int x) {
-          return &lds.half[((row_wave + h2 * kRowWaves) * (4 * kTok32) + x) * 64 + lane];
-        };
-        if (wave_live) {
+  // One tile: its scores; the next tile staged and a later one loaded, which the matrix
+  // instructions of the scores leave time for; the softmax and the second product. Loads are
+  // one or two tiles ahead of the staging, as registers allow.
+  // (Past the end of the look-up a tile is staged that nobody reads, and the last one
+  // loaded again.)
+  constexpr int kLoads = COLS == 128 ? 1 : 2;
+  const auto tile_step = [&](int i, int stop, int buf, Codes<COLS>& x) {
+    const int t = begin + i * TOK;
+    const uint64_t mask = ((1ull << kGroups) - 1) << ((i * kGroups) & 63);
+    const bool seen = t >= sight.all_lo && t + TOK <= sight.all_hi && (absent & mask) == 0;
+    if (!seen) take_out(i, buf);
+    const int ahead = i + 1 + kLoads < stop ? i + 1 + kLoads : stop - 1;
+    f32x16 sc[kTok32];
+    u32x4 f[kAhead];
+    if (wave_live) {
+      scores(sc, f, buf);
+      stage(i + 1, x, buf ^ 1);
+      load(ahead, x);
+    } else {
+      stage(i + 1, x, buf ^ 1);
+      load(ahead, x);
+    }
+    if constexpr (HALVES == 2) {
+      const auto place = [&](int h2, int x) {
+        return &lds.half[((row_wave + h2 * kRowWaves) * (4 * kTok32) + x) * 64 + lane];
+      };
+      if (wave_live) {
 #pragma unroll
-          for (int x = 0; x < 4 * kTok32; ++x)
-            *place(half, x) = f32x4{sc[x >> 2][4 * (x & 3)], sc[x >> 2][4 * (x & 3) + 1],
-                                    sc[x >> 2][4 * (x & 3) + 2], sc[x >> 2][4 * (x & 3) + 3]};
-        }
-        __syncthreads();
-        if (wave_live) {
-#pragma unroll
-          for (int x = 0; x < 4 * kTok32; ++x) {
-            const f32x4 o = *place(1 - half, x);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) sc[x >> 2][4 * (x & 3) + y] += o[y];
-          }
-          compute(sc, seen, i, i & 1);
-        }
-      }
-      if (i + 1 < stop) {
-        stage(i + 1, x, (i + 1) & 1);
-        if (i + 2 < stop) load(i + 2, x);
+        for (int x = 0; x < 4 * kTok32; ++x)
+          *place(half, x) = f32x4{sc[x >> 2][4 * (x & 3)], sc[x >> 2][4 * (x & 3) + 1],
+                                  sc[x >> 2][4 * (x & 3) + 2], sc[x >> 2][4 * (x & 3) + 3]};
       }
       __syncthreads();
+      if (wave_live) {
+#pragma unroll
+        for (int x = 0; x < 4 * kTok32; ++x) {
+          const f32x4 o = *place(1 - half, x);
+#pragma unroll
+          for (int y = 0; y < 4; ++y) sc[x >> 2][4 * (x & 3) + y] += o[y];
+        }
+      }
+    }
+    if (wave_live) compute(sc, f, seen, i, buf);
+    __syncthreads();
+  };
+  // Look-ups are for 64 groups; a tile's groups never straddle two of them.
+  for (int base = 0; base < tiles; base += kPerLook) {
+    look_up(begin + base * TOK);
+    const int stop = tiles - base < kPerLook ? tiles : base + kPerLook;
+    const auto last = [&](int i) { return i < stop ? i : stop - 1; };
+    Codes<COLS> x[kLoads];
+    load(base, x[0]);
+    if constexpr (kLoads == 2) load(last(base + 1), x[1]);
+    __syncthreads();
+    stage(base, x[0], 0);
+    load(last(base + kLoads), x[0]);
+    __syncthreads();
+    for (int i = base; i < stop; i += 2) {
+      tile_step(i, stop, 0, x[kLoads - 1]);
+      if (i + 1 < stop) tile_step(i + 1, stop, 1, x[0]);
     }
   }
 
   // results: the lane's columns 32 j + 8 b + 4 g + (0 .. 3) of row n
-  l += __shfl_xor(l, 32);
+  l = lane_sum<32>(l);
   if (live) {
     const RowPlace place = row_place(a, it, h, rho);
     const Part<kManyRows, D> part = part_of<kManyRows, D>(a, h, item);
@@ -496,10 +524,8 @@ __global__ __launch_bounds__(64 * kRowWaves * HALVES, 2) void qcache_any_rows_ke
 template <int TERMS, int D>
 hipError_t launch_qcache_any_rows(const QAttention& a, uint32_t many, uint32_t few,
                                   hipStream_t stream) {
-  // a wave's registers hold its queries' terms, d TERMS / 4 of them, and its columns of the output,
-  // d / 2; beyond 96 two waves share the rows
   constexpr int TOK = D == 256 ? 32 : 64;
-  constexpr int HALVES = D * (TERMS + 1) > 256 ? 2 : 1;
+  constexpr int HALVES = many_halves(D, TERMS);
   hipLaunchKernelGGL((qcache_any_rows_kernel<TERMS, D, TOK, HALVES>), dim3(many + few),
                      dim3(64 * kRowWaves * HALVES), 0, stream, a, many);
   return hipGetLastError();
