@@ -75,76 +75,38 @@ __device__ __forceinline__ u32x4 unit_codes(const u32x4 (&v)[ESIZE], float inv) 
   return out;
 }
 
-// One workgroup of four waves: 4 / TW tiles of TW waves, at the pages that begin in
-// window blockIdx.x of `window` tokens. UNITS: 16-element units of a lane.
+// One workgroup of four waves: 4 / TW tiles of TW waves, at the pages that begin in window
+// blockIdx.x of `window` tokens. UNITS: 16-element units of a lane.
 template <int ESIZE, int D, int TW, int UNITS>
 __global__ __launch_bounds__(256) void qcache_write_kernel(WriteArgs a, int32_t window) {
   __shared__ uint32_t s_max[2][4];
   constexpr int kUnitsPerRow = D / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int tl = threadIdx.x & (64 * TW - 1);   // thread of the tile
-  const int tile = (int)blockIdx.y * (4 / TW) + wave / TW;
+  const int tile = __builtin_amdgcn_readfirstlane((int)blockIdx.y * (4 / TW) + wave / TW);
   if (tile >= a.tiles) return;                  // (TW == 1: whole waves, no barrier below)
   const int h = tile % a.H, kv = (tile / a.H) & 1, layer = tile / (2 * a.H);
   const QRows rows = kv ? a.v : a.k;
   const int64_t slice = 2 * (int64_t)layer + kv;
-  uint8_t* codes = a.codes + slice * a.slice_codes;
-  float* scales = a.scales + slice * a.slice_scales;
   const uint8_t* src = rows.data + layer * rows.layer + h * rows.head;
   const int64_t B = (int64_t)1 << a.b_shift, n_slots = a.pages << a.b_shift;
-
-  const int64_t w0 = (int64_t)blockIdx.x * window;
-  const auto page_of = [&](int64_t i) -> int64_t {
-    const int64_t s = i >= 0 && i < a.n_tokens ? a.slots[i] : -1;
-    return s >= 0 && s < n_slots ? s >> a.b_shift : -1;
-  };
-  // the window's tokens that are the first of their page, skipped tokens aside
-  bool first = false;
-  if (lane < window) {
-    const int64_t p = page_of(w0 + lane);
-    if (p >= 0) {
-      int64_t j = w0 + lane - 1;
-      while (j >= 0 && page_of(j) < 0) --j;
-      first = page_of(j) != p;
-    }
-  }
-  uint64_t todo = __ballot(first);
   int turn = 0;
-  int64_t next = -1;                            // where the page goes on after skipped tokens
-  while (todo || next >= 0) {
-    const int64_t i = next >= 0 ? next : w0 + __builtin_ctzll(todo);
-    if (next < 0) todo &= todo - 1;
-    // the run of tokens in this page: lanes look at the next 128
-    const int64_t page = page_of(i);
-    const int row_lo = i + lane < a.n_tokens ? (int)(a.slots[i + lane] & (B - 1)) : 0;
-    const uint64_t same_lo = __ballot(page_of(i + lane) == page);
-    int count = ~same_lo ? __builtin_ctzll(~same_lo) : 64;
-    int row_hi = 0;
-    if (count == 64) {
-      const int64_t j = i + 64 + lane;
-      row_hi = j < a.n_tokens ? (int)(a.slots[j] & (B - 1)) : 0;
-      const uint64_t same_hi = __ballot(page_of(j) == page);
-      count += ~same_hi ? __builtin_ctzll(~same_hi) : 64;
-    }
-    count = count < B ? count : (int)B;
-    const int begin = __builtin_amdgcn_readfirstlane(row_lo);
-    next = i + count;
-    while (next < a.n_tokens && page_of(next) < 0) ++next;
-    if (next >= a.n_tokens || page_of(next) != page) next = -1;
 
+  // The `count` tokens of one page from i on, the first in row `begin` of it, token t in row
+  // row_of(t): loaded, their scale, their codes.
+  const auto write_page = [&](int64_t i, int64_t page, int count, int begin, auto row_of) {
+    float* scale_at = a.scales + slice * a.slice_scales + page * a.H + h;
+    uint8_t* codes = a.codes + slice * a.slice_codes + ((page * a.H + h) << a.b_shift) * D;
     u32x4 v[UNITS][ESIZE];
-    uint32_t top = 0;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int unit = u * 64 * TW + tl;
       const int t = unit / kUnitsPerRow, col = (unit % kUnitsPerRow) * 16;
-      if (t < count) {
-        const uint8_t* p = src + (i + t) * rows.token + col * ESIZE;
+      const uint8_t* at = src + (i + t) * rows.token + col * ESIZE;
 #pragma unroll
-        for (int w = 0; w < ESIZE; ++w) v[u][w] = *(global_ptr<u32x4>(p) + w);
-      } else {
-#pragma unroll
-        for (int w = 0; w < ESIZE; ++w) v[u][w] = u32x4{0, 0, 0, 0};
+      for (int w = 0; w < ESIZE; ++w) {
+        if (t < count) v[u][w] = *(global_ptr<u32x4>(at) + w);
+        else v[u][w] = u32x4{0, 0, 0, 0};
       }
     }
     const auto tile_max = [&](bool finite) -> uint32_t {
@@ -168,7 +130,7 @@ __global__ __launch_bounds__(256) void qcache_write_kernel(WriteArgs a, int32_t 
       }
       return m;
     };
-    top = tile_max(false);
+    uint32_t top = tile_max(false);
     if constexpr (TW == 2) {
       // two tiles share the workgroup's barriers: both look again if either has to
       bool again = false;
@@ -178,25 +140,22 @@ __global__ __launch_bounds__(256) void qcache_write_kernel(WriteArgs a, int32_t 
     } else {
       if (top >= 0x7F800000u) top = tile_max(true);
     }
-
-    float* scale_at = scales + page * a.H + h;
     float scale = __uint_as_float(scale_bits(top));
-    uint8_t* out = codes + ((page * a.H + h) << a.b_shift) * D;
     if (begin > 0) {
       const float old = *scale_at;
       const float grown = fmaxf(scale, old);
       if (grown > old) {
         const float ratio = old / grown;
         for (int unit = tl; unit < begin * kUnitsPerRow; unit += 64 * TW) {
-          u32x4* p = reinterpret_cast<u32x4*>(out) + unit;
-          u32x4 c = *p;
+          u32x4* at = reinterpret_cast<u32x4*>(codes) + unit;
+          u32x4 c = *at;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], false);
             const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], true);
             c[w] = codes_of(lo[0] * ratio, lo[1] * ratio, hi[0] * ratio, hi[1] * ratio);
           }
-          *p = c;
+          *at = c;
         }
       }
       scale = grown;
@@ -206,14 +165,85 @@ __global__ __launch_bounds__(256) void qcache_write_kernel(WriteArgs a, int32_t 
     for (int u = 0; u < UNITS; ++u) {
       const int unit = u * 64 * TW + tl;
       const int t = unit / kUnitsPerRow, col = (unit % kUnitsPerRow) * 16;
-      const int lo = __shfl(row_lo, t & 63), hi = __shfl(row_hi, t & 63);
+      const int row = row_of(t);
       if (t < count)
-        *reinterpret_cast<u32x4*>(out + (t < 64 ? lo : hi) * D + col) =
-            unit_codes<ESIZE>(v[u], inv);
+        *reinterpret_cast<u32x4*>(codes + row * D + col) = unit_codes<ESIZE>(v[u], inv);
     }
     if constexpr (TW > 1) __syncthreads();      // every wave has read the old scale
     if (tl == 0) *scale_at = scale;
-    if (next >= 0) {                            // the tile is read again
+  };
+
+  const int64_t w0 = (int64_t)blockIdx.x * window;
+  // Lanes look at the tokens from the one before the window on: with pages of at most 32
+  // tokens 64 of them hold every page that begins in the window, unless tokens are skipped.
+  if (B <= 32) {
+    const int64_t at = w0 - 1 + lane;
+    const int64_t s = at >= 0 && at < a.n_tokens ? a.slots[at] : -1;
+    const int page = s >= 0 && s < n_slots ? (int)(s >> a.b_shift) : -1;
+    const int row = (int)(s & (B - 1));
+    const int before = __shfl_up(page, 1);
+    const uint64_t skipped = __ballot(at >= 0 && at < a.n_tokens && page < 0);
+    uint64_t first = __ballot(lane >= 1 && lane <= window && page >= 0 && page != before);
+    bool simple = skipped == 0;
+    for (uint64_t f = first; f && simple; f &= f - 1) {
+      const int l = __builtin_ctzll(f);
+      const uint64_t other = ~__ballot(page == __builtin_amdgcn_readlane(page, l)) >> l;
+      simple = other && __builtin_ctzll(other) <= B;
+    }
+    if (simple) {
+      for (; first; first &= first - 1) {
+        const int l = __builtin_ctzll(first);
+        const int here = __builtin_amdgcn_readlane(page, l);
+        const uint64_t other = ~__ballot(page == here) >> l;
+        write_page(w0 - 1 + l, here, __builtin_ctzll(other), __builtin_amdgcn_readlane(row, l),
+                   [&](int t) { return __shfl(row, (l + t) & 63); });
+      }
+      return;
+    }
+  }
+
+  // Pages of any length, with skipped tokens.
+  const auto page_of = [&](int64_t i) -> int64_t {
+    const int64_t s = i >= 0 && i < a.n_tokens ? a.slots[i] : -1;
+    return s >= 0 && s < n_slots ? s >> a.b_shift : -1;
+  };
+  // the window's tokens that are the first of their page, skipped tokens aside
+  bool first = false;
+  if (lane < window) {
+    const int64_t p = page_of(w0 + lane);
+    if (p >= 0) {
+      int64_t j = w0 + lane - 1;
+      while (j >= 0 && page_of(j) < 0) --j;
+      first = page_of(j) != p;
+    }
+  }
+  uint64_t todo = __ballot(first);
+  int64_t next = -1;                            // where the page goes on after skipped tokens
+  while (todo || next >= 0) {
+    const int64_t i = next >= 0 ? next : w0 + __builtin_ctzll(todo);
+    if (next < 0) todo &= todo - 1;
+    // the run of tokens in this page: lanes look at the next 128
+    const int64_t page = page_of(i);
+    const int row_lo = i + lane < a.n_tokens ? (int)(a.slots[i + lane] & (B - 1)) : 0;
+    const uint64_t same_lo = __ballot(page_of(i + lane) == page);
+    int count = ~same_lo ? __builtin_ctzll(~same_lo) : 64;
+    int row_hi = 0;
+    if (count == 64) {
+      const int64_t j = i + 64 + lane;
+      row_hi = j < a.n_tokens ? (int)(a.slots[j] & (B - 1)) : 0;
+      const uint64_t same_hi = __ballot(page_of(j) == page);
+      count += ~same_hi ? __builtin_ctzll(~same_hi) : 64;
+    }
+    count = count < B ? count : (int)B;
+    const int begin = __builtin_amdgcn_readfirstlane(row_lo);
+    next = i + count;
+    while (next < a.n_tokens && page_of(next) < 0) ++next;
+    if (next >= a.n_tokens || page_of(next) != page) next = -1;
+    write_page(i, page, count, begin, [&](int t) {
+      const int lo = __shfl(row_lo, t & 63), hi = __shfl(row_hi, t & 63);
+      return t < 64 ? lo : hi;
+    });
+    if (next >= 0) {                            // the tiles are read again
       __threadfence_block();
       if constexpr (TW > 1) __syncthreads();
     }
@@ -240,7 +270,12 @@ hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t
   a.b_shift = c.b_shift;
   a.tiles = n_layers * 2 * c.H;
   const int32_t B = 1 << c.b_shift;
-  const int32_t window = n_tokens * a.tiles <= (1 << 14) ? 1 : (B < 64 ? B : 64);
+  // Few rows (decoding steps): a window of one token, so that every page has waves of its own.
+  // Many: as many tokens as the lanes can look at with the pages that begin among them, at
+  // most 32, since a wave without a page would only be in the way (the 4B-N4 merged
+  // cache by windows of 16 tokens 709 us, of 32 668; its pages by one token 880).
+  const bool bulk = n_tokens * a.tiles > (1 << 14);
+  const int32_t window = !bulk ? 1 : B == 32 ? 31 : 32;
   const int64_t windows = (n_tokens + window - 1) / window;
   ScopedTiming tm(K_QCACHE_WRITE, stream);
   const auto go = [&](auto e, auto dd, auto tw, auto units) {
