@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPer = CM_QCACHE_MAX_REQUESTS / kThreads;  // requests of one thread's scan
-constexpr int kTokensPerGroup = 2048;
+constexpr int kTokensPerGroup = 512;  // two a thread: 262144 tokens 6.9 us, by eight 11.8
 
 struct Sum2 {
   int64_t tokens, pages;
