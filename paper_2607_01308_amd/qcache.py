@@ -11,6 +11,7 @@ in use there and does not wait: lengths, tables and slots stay on the device."""
 from __future__ import annotations
 
 import ctypes
+from contextlib import nullcontext
 from dataclasses import dataclass
 from typing import Dict, Optional, Sequence
 
@@ -56,11 +57,20 @@ class QCache:
                 f"device={self.device})")
 
 
+def _stream(stream, device):
+    return stream if stream is not None else torch.cuda.current_stream(device)
+
+
+def _made_on(stream):
+    """Where tensors that a call makes are allocated: on the stream it enqueues on."""
+    return nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _use(stream, device, *tensors) -> ctypes.c_void_p:
     """The stream a call enqueues on, with the tensors its kernels read and write
     marked as in use there: their memory must not go to another tensor before that
     work has finished, whichever stream they were allocated on."""
-    s = stream if stream is not None else torch.cuda.current_stream(device)
+    s = _stream(stream, device)
     for t in tensors:
         if t is not None:
             t.record_stream(s)
@@ -116,34 +126,32 @@ def qcache_tables(pages: int, block: int, held: torch.Tensor, new: torch.Tensor,
     _check(held, "held", i32, dev, (n,))
     _check(new, "new", i32, dev, (n,))
     _check(free, "free", i32, dev)
-    s = stream if stream is not None else torch.cuda.current_stream(dev)
-    with torch.cuda.stream(s):
-        # slots and info, then rows and lens, in one buffer
-        buf = torch.empty(tokens + 4 + n + 1, dtype=torch.int64, device=dev)
-        small = buf[tokens + 4:].view(i32)
-        step = QCacheStep(buf[:tokens], small[:n + 1], small[n + 1:2 * n + 1],
-                          buf[tokens:tokens + 4])
-    _use(s, dev, held, new, free, table)
-    base = buf.data_ptr()
+    with _made_on(stream):
+        step = QCacheStep(torch.empty(tokens, dtype=torch.int64, device=dev),
+                          torch.empty(n + 1, dtype=i32, device=dev),
+                          torch.empty(n, dtype=i32, device=dev),
+                          torch.empty(4, dtype=torch.int64, device=dev))
+    s = _use(stream, dev, held, new, free, table)
     C.check(C.lib().cm_qcache_tables(
         pages, block, n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
-        table.data_ptr(), width, tokens, base, base + 8 * (tokens + 4),
-        base + 8 * (tokens + 4) + 4 * (n + 1), base + 8 * tokens, s.cuda_stream),
-        "cm_qcache_tables")
+        table.data_ptr(), width, tokens, step.slots.data_ptr(), step.rows.data_ptr(),
+        step.lens.data_ptr(), step.info.data_ptr(), s.cuda_stream), "cm_qcache_tables")
     return step
 
 
 def _rows(x: torch.Tensor, name: str, cache: QCache, tokens: int):
-    if x.dim() == 3:
-        x = x.unsqueeze(0)
-    if x.dim() != 4 or x.shape[1:] != (tokens, cache.H, cache.d):
+    """The layers of x and its rows as the library takes them."""
+    shape, stride = x.shape, x.stride()
+    if len(shape) == 3:
+        shape, stride = (1, *shape), (0, *stride)
+    if len(shape) != 4 or shape[1:] != (tokens, cache.H, cache.d):
         raise ValueError(f"{name} must be [layers, {tokens}, {cache.H}, {cache.d}], got "
                          f"{list(x.shape)}")
     if x.device != cache.device:
         raise ValueError(f"{name} must live on {cache.device}")
-    if x.stride(3) != 1:
+    if stride[3] != 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
-    return x, C.CmQrows(x.data_ptr(), x.stride(0), x.stride(1), x.stride(2))
+    return shape[0], C.CmQrows(x.data_ptr(), *stride[:3])
 
 
 def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
@@ -153,14 +161,14 @@ def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
     dimension, in multiples of 16 bytes."""
     tokens = slots.numel()
     _check(slots, "slots", torch.int64, cache.device)
-    kt, kr = _rows(k, "k", cache, tokens)
-    vt, vr = _rows(v, "v", cache, tokens)
+    layers, kr = _rows(k, "k", cache, tokens)
+    v_layers, vr = _rows(v, "v", cache, tokens)
     if k.dtype not in _DTYPES or v.dtype is not k.dtype:
         raise TypeError(f"k and v must both be bfloat16 or float32, got {k.dtype} and {v.dtype}")
-    if kt.shape[0] != vt.shape[0]:
+    if layers != v_layers:
         raise ValueError("k and v must have the same layers")
     s = _use(stream, cache.device, cache.codes, cache.scales, k, v, slots)
-    C.check(C.lib().cm_qcache_write(ctypes.byref(cache.struct), layer, kt.shape[0],
+    C.check(C.lib().cm_qcache_write(ctypes.byref(cache.struct), layer, layers,
                                     _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens,
                                     slots.data_ptr(), s.cuda_stream), "cm_qcache_write")
 
@@ -219,9 +227,8 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         _check(rows, "rows", torch.int32, dev, (n + 1,))
     if max_rows is None:
         max_rows = 1 if rows is None else n_rows
-    s = stream if stream is not None else torch.cuda.current_stream(dev)
     if out is None or lse is None:
-        with torch.cuda.stream(s):
+        with _made_on(stream):
             if out is None:
                 out = torch.empty((n_rows, q_heads, d), dtype=q.dtype, device=dev)
             if lse is None:
@@ -234,8 +241,8 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         d ** -0.5 if scale is None else scale, q.data_ptr(), q.stride(0), q.stride(1),
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
+    s = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
     ws = _workspace(cache, step, s)
-    _use(s, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
     C.check(C.lib().cm_qcache_attention(ctypes.byref(cache.struct), layer, ctypes.byref(step),
                                         ws.data_ptr(), ws.numel(), s.cuda_stream),
             "cm_qcache_attention")
