@@ -314,20 +314,25 @@ __device__ __forceinline__ void get_part(const float* at, float& x, float& y) {
   y = __uint_as_float(w[1]);
 }
 
-// Partial results of an item: ROWS rows of D values, then the exponent m and the sum l of
-// each row: of the item, and of the group that it is the first of.
+// Partial results of an item: `rows` rows of D values, then the exponent m and the sum l of
+// each row: of the item, and of the group that it is the first of. The values are stored as
+// the lanes hold them, two columns of one row after another: a store of a wave fills whole
+// lines (row after row it was 8 bytes of 64 lines, which such stores write one by one).
 template <int ROWS, int D>
 struct Part {
   static constexpr int64_t kFloats = (int64_t)ROWS * (D + 4);
   float* at;
+  int rows;
   __device__ __forceinline__ void put_quad(int row, int q, f32x4 v) const {
-    put_part(at + row * D + 4 * q, v[0], v[1]);
-    put_part(at + row * D + 4 * q + 2, v[2], v[3]);
+    float* p = at + 2 * (2 * q * rows + row);
+    put_part(p, v[0], v[1]);
+    put_part(p + 2 * rows, v[2], v[3]);
   }
   __device__ __forceinline__ f32x4 quad(int row, int q) const {
+    const float* p = at + 2 * (2 * q * rows + row);
     float x[4];
-    get_part(at + row * D + 4 * q, x[0], x[1]);
-    get_part(at + row * D + 4 * q + 2, x[2], x[3]);
+    get_part(p, x[0], x[1]);
+    get_part(p + 2 * rows, x[2], x[3]);
     return f32x4{x[0], x[1], x[2], x[3]};
   }
   __device__ __forceinline__ void put_stat(int level, int row, float m, float l) const {
@@ -338,10 +343,13 @@ struct Part {
   }
 };
 template <int ROWS, int D>
-__device__ __forceinline__ Part<ROWS, D> part_of(const QAttention& a, int h, int item) {
+__device__ __forceinline__ Part<ROWS, D> part_of(const QAttention& a, const Item& it, int h,
+                                                 int place) {
   constexpr bool kFew = ROWS == kFewRows;
+  const int rows = it.count * a.G - it.tile * ROWS;
   return {(kFew ? a.few_part : a.many_part) +
-          ((int64_t)h * (kFew ? a.few_max : a.many_max) + item) * Part<ROWS, D>::kFloats};
+              ((int64_t)h * (kFew ? a.few_max : a.many_max) + place) * Part<ROWS, D>::kFloats,
+          rows < ROWS ? rows : ROWS};
 }
 
 // Four columns of a row while they are joined from partial results.
@@ -377,9 +385,8 @@ template <int ROWS, int D, int ES, int THREADS, int BATCH, int QUADS, class Slot
 __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, int h, int count,
                                           int level, bool whole, Slot slot) {
   constexpr int kQuads = D / 4;
-  const int left = it.count * a.G - it.tile * ROWS;
-  const int total = (left < ROWS ? left : ROWS) * kQuads;
-  const Part<ROWS, D> p0 = part_of<ROWS, D>(a, h, slot(0));
+  const Part<ROWS, D> p0 = part_of<ROWS, D>(a, it, h, slot(0));
+  const int total = p0.rows * kQuads;
   for (int x0 = threadIdx.x; x0 < total; x0 += THREADS * QUADS) {
     Joined sum[QUADS];
     for (int s = 0; s < count; s += BATCH) {
@@ -387,12 +394,13 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
       float m[QUADS][BATCH], l[QUADS][BATCH];
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
-        const Part<ROWS, D> p = part_of<ROWS, D>(a, h, slot(s + k < count ? s + k : s));
+        const Part<ROWS, D> p = part_of<ROWS, D>(a, it, h, slot(s + k < count ? s + k : s));
 #pragma unroll
         for (int u = 0; u < QUADS; ++u) {
           const int x = x0 + u * THREADS < total ? x0 + u * THREADS : x0;
-          o[u][k] = p.quad(x / kQuads, x % kQuads);
-          p.stat(level, x / kQuads, m[u][k], l[u][k]);
+          const int quad = (int)((uint32_t)x / (uint32_t)p.rows), row = x - quad * p.rows;
+          o[u][k] = p.quad(row, quad);
+          p.stat(level, row, m[u][k], l[u][k]);
         }
       }
 #pragma unroll
@@ -411,7 +419,7 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
     for (int u = 0; u < QUADS; ++u) {
       const int x = x0 + u * THREADS;
       if (x >= total) break;
-      const int row = x / kQuads, quad = x % kQuads;
+      const int quad = (int)((uint32_t)x / (uint32_t)p0.rows), row = x - quad * p0.rows;
       if (whole) {
         const RowPlace place = row_place(a, it, h, it.tile * ROWS + row);
         put_quad<ES>(a, place, 4 * quad, sum[u].o, sum[u].l);

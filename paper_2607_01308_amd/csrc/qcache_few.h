@@ -319,7 +319,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
     __syncthreads();
   }
   if (wave == 0 && live) {
-    const Part<kFewRows, D> part = part_of<kFewRows, D>(a, h, slot);
+    const Part<kFewRows, D> part = part_of<kFewRows, D>(a, it, h, slot);
     const RowPlace place = row_place(a, it, h, rho);
 #pragma unroll
     for (int i = 0; i < 4; ++i)

@@ -483,7 +483,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   l = lane_sum<32>(l);
   if (live) {
     const RowPlace place = row_place(a, it, h, rho);
-    const Part<kManyRows, D> part = part_of<kManyRows, D>(a, h, item);
+    const Part<kManyRows, D> part = part_of<kManyRows, D>(a, it, h, item);
     const int row = row_wave * kWaveRows + n;
 #pragma unroll
     for (int j = 0; j < DH / 32; ++j)

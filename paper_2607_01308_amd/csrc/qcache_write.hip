@@ -10,6 +10,7 @@
 // two and rounded again.
 //
 // Bound by bandwidth: each row is read once and its codes are written once.
+#include <algorithm>
 #include <type_traits>
 
 #include "qcache_ops.h"
@@ -24,6 +25,7 @@ struct WriteArgs {
   float* scales;
   int64_t slice_codes, slice_scales;  // of one (layer, K/V)
   int64_t pages, n_tokens;
+  int64_t from;                       // first token of the launch's windows
   const int64_t* slots;
   int32_t H, b_shift, tiles;          // tiles: layers * 2 * H of a page
 };
@@ -76,7 +78,7 @@ __device__ __forceinline__ u32x4 unit_codes(const u32x4 (&v)[ESIZE], float inv) 
 }
 
 // One workgroup of four waves: 4 / TW tiles of TW waves, at the pages that begin in window
-// blockIdx.x of `window` tokens. UNITS: 16-element units of a lane.
+// blockIdx.x of `window` tokens, a.from on. UNITS: 16-element units of a lane.
 template <int ESIZE, int D, int TW, int UNITS>
 __global__ __launch_bounds__(256) void qcache_write_kernel(WriteArgs a, int32_t window) {
   __shared__ uint32_t s_max[2][4];
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(256) void qcache_write_kernel(WriteArgs a, int32_t 
     if (tl == 0) *scale_at = scale;
   };
 
-  const int64_t w0 = (int64_t)blockIdx.x * window;
+  const int64_t w0 = a.from + (int64_t)blockIdx.x * window;
   // Lanes look at the tokens from the one before the window on: with pages of at most 32
   // tokens 64 of them hold every page that begins in the window, unless tokens are skipped.
   if (B <= 32) {
@@ -281,9 +283,14 @@ hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t
   const auto go = [&](auto e, auto dd, auto tw, auto units) {
     constexpr int ESIZE = decltype(e)::value, D = decltype(dd)::value, TW = decltype(tw)::value,
                   UNITS = decltype(units)::value;
-    const dim3 grid((uint32_t)windows, (uint32_t)((a.tiles + 4 / TW - 1) / (4 / TW)));
-    hipLaunchKernelGGL((qcache_write_kernel<ESIZE, D, TW, UNITS>), grid, dim3(256), 0, stream, a,
-                       window);
+    // a launch holds at most 2^24 - 1 workgroups of 256 threads a row of the grid
+    for (int64_t done = 0; done < windows; done += (1 << 24) - 1) {
+      const int64_t some = std::min<int64_t>(windows - done, (1 << 24) - 1);
+      const dim3 grid((uint32_t)some, (uint32_t)((a.tiles + 4 / TW - 1) / (4 / TW)));
+      a.from = done * window;
+      hipLaunchKernelGGL((qcache_write_kernel<ESIZE, D, TW, UNITS>), grid, dim3(256), 0, stream,
+                         a, window);
+    }
   };
   const auto by_type = [&](auto dd, auto tw, auto units) {
     if (dtype == CM_BF16) go(std::integral_constant<int, 2>{}, dd, tw, units);
