@@ -352,6 +352,20 @@ __device__ __forceinline__ Part<ROWS, D> part_of(const QAttention& a, const Item
           rows < ROWS ? rows : ROWS};
 }
 
+// x, of which the compiler does not know that it is x: what is computed from it is computed where
+// it is used, not kept in registers.
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The lane's number, computed where it is asked for.
+__device__ __forceinline__ int lane_anew() {
+  int all = -1;
+  asm volatile("" : "+s"(all));
+  return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)all, __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+}
+
 // Four columns of a row while they are joined from partial results.
 struct Joined {
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -387,7 +401,7 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
   constexpr int kQuads = D / 4;
   const Part<ROWS, D> p0 = part_of<ROWS, D>(a, it, h, slot(0));
   const int total = p0.rows * kQuads;
-  for (int x0 = threadIdx.x; x0 < total; x0 += THREADS * QUADS) {
+  for (int x0 = anew(threadIdx.x); x0 < total; x0 += THREADS * QUADS) {
     Joined sum[QUADS];
     for (int s = 0; s < count; s += BATCH) {
       f32x4 o[QUADS][BATCH];

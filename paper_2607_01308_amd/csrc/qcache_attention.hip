@@ -13,7 +13,7 @@ constexpr int kFewWaves = 4;
 
 template <int TERMS, int D>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void qcache_few_rows_kernel(QAttention a) {
-  __shared__ FewShared<D, kFewWaves> lds;
+  __shared__ FewShared<TERMS, D, kFewWaves> lds;
   few_rows_span<TERMS, D, kFewWaves>(a, blockIdx.x, lds);
 }
 

@@ -54,9 +54,14 @@ __device__ __forceinline__ void load_columns(uint32_t (&dst)[D / 64], const uint
   }
 }
 
+// Whether the queries lie in the LDS: three terms of d = 256 are 96 registers a lane, for which
+// there is no room (spilled, 64 contexts of 8192 tokens of 4 heads took 261 us, not 208).
+constexpr bool shared_query(int terms, int d) { return terms * d > 512; }
+
 // What the threads of a workgroup share.
-template <int D, int WAVES>
+template <int TERMS, int D, int WAVES>
 struct FewShared {
+  bf16x8 q[shared_query(TERMS, D) ? D / 32 * TERMS * 64 : 1];  // [chunk][term][lane]
   float acc[WAVES / 2][kFewRows][D + 4];         // results of the waves, at a segment's end
   float m[WAVES / 2][kFewRows], l[WAVES / 2][kFewRows];
   int pos[CM_QCACHE_MAX_REQUESTS + 1];           // where the requests begin, in units
@@ -74,11 +79,13 @@ __device__ __forceinline__ int few_units(const QAttention& a, int count, int len
 
 template <int TERMS, int D, int WAVES>
 __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item& it, int h, int slot,
-                                                 FewShared<D, WAVES>& lds) {
+                                                 FewShared<TERMS, D, WAVES>& lds) {
   constexpr int DW = D / 16;                     // columns of a lane
   constexpr int ES = TERMS == 1 ? 2 : 4;         // bytes of a query element
   constexpr int PT = TERMS == 1 ? 2 : 3;         // terms of a probability
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // (The lane's numbers are made anew for each segment and for its end: addresses made from
+  // them before would be kept in registers through the loop, which for d = 256 has none left.)
+  const int lane = anew(threadIdx.x & 63), wave = threadIdx.x >> 6;
   const int n = lane & 15, g = lane >> 4;
 
   // the lane's query row
@@ -101,11 +108,23 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
   begin += wave * share;
   end = end < begin + share ? end : begin + share;
 
-  bf16x8 q[D / 32][TERMS];
+  // elements of chunk c / 2, half c % 2, in the order of the K codes that a lane holds
+  const auto query = [&](int c, bf16x8 (&dst)[TERMS]) {
+    load_query<TERMS>(a, it.row0 + tok, head, (c >> 1) * 64 + g * 16 + (c & 1) * 8, live, dst);
+  };
+  constexpr bool kShared = shared_query(TERMS, D);
+  bf16x8 q[kShared ? 1 : D / 32][TERMS];
+  if constexpr (kShared) {
+    for (int c = wave; c < D / 32; c += WAVES) {
+      query(c, q[0]);
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c)
-    // elements of chunk c / 2, half c % 2, in the order of the K codes that a lane holds
-    load_query<TERMS>(a, it.row0 + tok, head, (c >> 1) * 64 + g * 16 + (c & 1) * 8, live, q[c]);
+      for (int w = 0; w < TERMS; ++w) lds.q[(c * TERMS + w) * 64 + lane] = q[0][w];
+    }
+    __syncthreads();                             // (its readers end at the barriers below)
+  } else {
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) query(c, q[c]);
+  }
 
   f32x4 acc[DW];                                 // acc[j][i]: column (4g + i) * D / 16 + j of row n
 #pragma unroll
@@ -159,6 +178,11 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
     for (int s = 0; s < steps; ++s) {
       const int t = t0 + s * kStep;
       f32x4 sc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+      const int q_lane = kShared ? anew(lane) : lane;
+      const auto of_query = [&](int c, int w) {
+        if constexpr (kShared) return lds.q[(c * TERMS + w) * 64 + q_lane];
+        else return q[c][w];
+      };
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
 #pragma unroll
@@ -168,7 +192,8 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
             const bf16x8 k = operand(x.k[b][c][2 * half], x.k[b][c][2 * half + 1]);
 #pragma unroll
             for (int w = TERMS - 1; w >= 0; --w)
-              sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[2 * c + half][w], sc[b], 0, 0, 0);
+              sc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, of_query(2 * c + half, w), sc[b],
+                                                              0, 0, 0);
           }
         }
       }
@@ -209,29 +234,28 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
             by[k] = ((sees >> (2 * k)) & 1 ? 0x3F80u : 0u) |
                     ((sees >> (2 * k + 1)) & 1 ? 0x3F800000u : 0u);
 #pragma unroll
-          for (int j = 0; j < DW; ++j) {
-            u32x4 is;                            // 1 where the code is NaN
+          for (int w = 0; w < D / 64; ++w) {
+            uint32_t bad[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t lo = nan_codes(x.v[k >> 1][2 * (k & 1)][j >> 2]) >> (8 * (j & 3));
-              const uint32_t hi2 = nan_codes(x.v[k >> 1][2 * (k & 1) + 1][j >> 2]) >> (8 * (j & 3));
-              is[k] = (lo & 1) * 0x3F80u | (hi2 & 1) * 0x3F800000u;
+            for (int k = 0; k < 8; ++k) bad[k] = nan_codes((uint32_t)anew((int)x.v[k >> 2][k & 3][w]));
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+              u32x4 is;                          // 1 where the code is NaN
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                is[k] = ((bad[2 * k] >> (8 * o)) & 1) * 0x3F80u |
+                        ((bad[2 * k + 1] >> (8 * o)) & 1) * 0x3F800000u;
+              f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+              hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is),
+                                                             __builtin_bit_cast(bf16x8, by), hits, 0,
+                                                             0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (hits[i] > 0.f) acc[4 * w + o][i] = __builtin_nanf("");
             }
-            f32x4 hits = {0.f, 0.f, 0.f, 0.f};
-            hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is),
-                                                           __builtin_bit_cast(bf16x8, by), hits, 0,
-                                                           0, 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (hits[i] > 0.f) acc[j][i] = __builtin_nanf("");
+            for (int k = 0; k < 8; ++k) x.v[k >> 2][k & 3][w] &= ~(bad[k] * 0xFFu);
           }
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-#pragma unroll
-            for (int w = 0; w < D / 64; ++w) {
-              uint32_t& c = x.v[k >> 2][k & 3][w];
-              c &= ~(nan_codes(c) * 0xFFu);
-            }
         }
       }
       float best = e[0];
@@ -286,30 +310,31 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
 
   // the waves' results as one, half of the waves to the other half at a time
   l = lane_sum<32>(lane_sum<16>(l));
+  const int en = anew(n), eg = anew(g);
 #pragma unroll
   for (int half = WAVES / 2; half >= 1; half >>= 1) {
     if (wave >= half && wave < 2 * half) {
       const int to = wave - half;
-      float* row = &lds.acc[to][n][4 * g * DW];
+      float* row = &lds.acc[to][en][4 * eg * DW];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < DW; j += 4)
           *reinterpret_cast<f32x4*>(&row[i * DW + j]) =
               f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
-      if (g == 0) {
-        lds.m[to][n] = top;
-        lds.l[to][n] = l;
+      if (eg == 0) {
+        lds.m[to][en] = top;
+        lds.l[to][en] = l;
       }
     }
     __syncthreads();
     if (wave < half) {
-      const float* row = &lds.acc[wave][n][4 * g * DW];
-      const float m = fmaxf(top, lds.m[wave][n]);
+      const float* row = &lds.acc[wave][en][4 * eg * DW];
+      const float m = fmaxf(top, lds.m[wave][en]);
       const float low = m == kNone ? 0.f : m;
       const float mine = __builtin_amdgcn_exp2f(top - low);
-      const float other = __builtin_amdgcn_exp2f(lds.m[wave][n] - low);
-      l = l * mine + other * lds.l[wave][n];
+      const float other = __builtin_amdgcn_exp2f(lds.m[wave][en] - low);
+      l = l * mine + other * lds.l[wave][en];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -320,19 +345,19 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
   }
   if (wave == 0 && live) {
     const Part<kFewRows, D> part = part_of<kFewRows, D>(a, it, h, slot);
-    const RowPlace place = row_place(a, it, h, rho);
+    const RowPlace place = row_place(a, it, h, it.tile * kFewRows + en);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < DW; j += 4) {
         const f32x4 y = {acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
-        const int col = (4 * g + i) * DW + j;
+        const int col = (4 * eg + i) * DW + j;
         if (it.splits == 1) put_quad<ES>(a, place, col, y, l);
-        else part.put_quad(n, col / 4, y);
+        else part.put_quad(en, col / 4, y);
       }
-    if (g == 0) {
+    if (eg == 0) {
       if (it.splits == 1) put_lse(a, place, top == kNone ? 0.f : top, l);
-      else part.put_stat(0, n, top, l);
+      else part.put_stat(0, en, top, l);
     }
   }
 }
@@ -340,7 +365,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
 // The segments of a workgroup's span, one after another.
 template <int TERMS, int D, int WAVES>
 __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
-                                              FewShared<D, WAVES>& lds) {
+                                              FewShared<TERMS, D, WAVES>& lds) {
   constexpr int ES = TERMS == 1 ? 2 : 4;
   constexpr int kThreads = 64 * WAVES, kPer = CM_QCACHE_MAX_REQUESTS / kThreads;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;

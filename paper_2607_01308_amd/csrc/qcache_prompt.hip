@@ -60,13 +60,19 @@ struct Codes {
   uint32_t v[COLS / 16];
 };
 
+// 16-column chunks of its queries that a wave keeps in the LDS: three terms of 128 columns
+// leave no registers for the last two.
+constexpr int shared_chunks(int terms, int columns) { return terms * columns > 256 ? 2 : 0; }
+
 // The LDS of a workgroup.
-template <int D, int TOK, int HALVES>
+template <int TERMS, int D, int TOK, int HALVES>
 struct ManyShared {
   uint8_t k[2][D * TOK * 2];
   uint8_t v[2][D * TOK * 2];
   // halves of scores that waves exchange
   f32x4 half[HALVES == 2 ? kRowWaves * HALVES * (TOK / 32) * 4 * 64 : 1];
+  static constexpr int kQuery = shared_chunks(TERMS, D / HALVES) * TERMS;
+  bf16x8 q[kQuery ? kRowWaves * HALVES * kQuery * 64 : 1];  // [wave][chunk][term][lane]
   FindShared find;
   int flag;
 };
@@ -75,7 +81,7 @@ struct ManyShared {
 // they exchange through the LDS, and half of the output's columns.
 template <int TERMS, int D, int TOK, int HALVES>
 __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
-                                               ManyShared<D, TOK, HALVES>& lds) {
+                                               ManyShared<TERMS, D, TOK, HALVES>& lds) {
   using T = Tile<D, TOK>;
   constexpr int kWaves = kRowWaves * HALVES;
   constexpr int DH = D / HALVES;                 // columns of a wave
@@ -100,7 +106,8 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const int head = h * a.G + rho % a.G;
   const int p = it.len - it.count + tok;
   const int see_hi = live && p >= 0 ? p + 1 : 0;
-  const int see_lo = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+  // (from see_hi where it is asked for: one register less through the tiles)
+  const auto see_from = [&] { return a.window && see_hi > a.window ? see_hi - a.window : 0; };
   const Sight sight = tile_sight<kManyRows>(a, it);
   const bool wave_live = it.tile * kManyRows + row_wave * kWaveRows < it.count * a.G;
 
@@ -110,10 +117,19 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   end = end < sight.any_hi ? end : sight.any_hi;
   const int tiles = end > begin ? (end - begin + TOK - 1) / TOK : 0;
 
-  bf16x8 q[DH / 16][TERMS];
+  constexpr int kKept = DH / 16 - shared_chunks(TERMS, DH);
+  bf16x8 q[kKept][TERMS];
 #pragma unroll
-  for (int c = 0; c < DH / 16; ++c)
+  for (int c = 0; c < kKept; ++c)
     load_query<TERMS>(a, it.row0 + tok, head, half * DH + c * 16 + g * 8, live, q[c]);
+  const uint32_t q_place = wave * lds.kQuery * 64 + lane;
+#pragma unroll
+  for (int c = kKept; c < DH / 16; ++c) {
+    bf16x8 x[TERMS];
+    load_query<TERMS>(a, it.row0 + tok, head, half * DH + c * 16 + g * 8, live, x);
+#pragma unroll
+    for (int w = 0; w < TERMS; ++w) lds.q[q_place + ((c - kKept) * TERMS + w) * 64] = x[w];
+  }
 
   f32x16 acc[DH / 32];
 #pragma unroll
@@ -136,7 +152,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   float my_kf = 0.f, my_vl = 0.f, my_vi = 1.f;   // scores' factor; log2 and inverse of V's rest
   uint64_t absent = 0;
   const auto look_up = [&](int t0) {
-    const int my_t = t0 + lane * 16;
+    const int my_t = t0 + lane_anew() * 16;
     bool there = false;
     my_page = 0;
     float ks = 1.f, vs = 1.f;
@@ -167,18 +183,21 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   // four columns) or, for 64 columns, (tokens 4 (lane / 16) + i, four columns).
   const uint32_t k_load = (lane >> 2) * D + (lane & 3) * (COLS / 4) + col0;
   const uint32_t v_load = (COLS == 128 ? 4 * g * D + 4 * n : 4 * (lane >> 4) * D + 4 * (lane & 15)) + col0;
+  // (what is made of it is computed again for each tile, not kept for all of them in registers)
+  const auto fresh = [](uint32_t x) { return (uint32_t)anew((int)x); };
   const auto load = [&](int tile, Codes<COLS>& x) {
+    const uint32_t kl = fresh(k_load), vl = fresh(v_load);
     const int gi = (tile * kGroups + my_group) & 63;
     const int64_t page = __builtin_amdgcn_readlane(my_page, gi);
     const int row = __builtin_amdgcn_readfirstlane((begin + tile * TOK + my_group * 16) & (B - 1));
     const int64_t base = page * page_codes + head_codes + (int64_t)row * D;
     const uint8_t* kp = a.kc + base;
 #pragma unroll
-    for (int w = 0; w < COLS / 64; ++w) x.k[w] = *global_ptr<u32x4>(kp + (k_load + 16 * w));
+    for (int w = 0; w < COLS / 64; ++w) x.k[w] = *global_ptr<u32x4>(kp + (kl + 16 * w));
     const uint8_t* vp = a.vc + base;
 #pragma unroll
     for (int i = 0; i < COLS / 16; ++i)
-      x.v[i] = *global_ptr<uint32_t>(vp + (v_load + ((i & 3) + 8 * (i >> 2)) * D));
+      x.v[i] = *global_ptr<uint32_t>(vp + (vl + ((i & 3) + 8 * (i >> 2)) * D));
   };
   // A lane's places in the LDS: what it reads of K and V, what it stages of them.
   const uint32_t k_read = T::k_at(n, half * (DH / 8) + g);
@@ -189,11 +208,6 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       COLS == 128 ? T::v_at(col0 + 4 * n, 2 * my_group + g)
                   : T::v_at(col0 + 4 * (lane & 15), 2 * my_group + ((lane >> 4) & 1)) +
                         8 * (lane >> 5);
-  // (opaque: computed again for each tile, not kept for all of them in registers)
-  const auto fresh = [](uint32_t x) {
-    asm volatile("" : "+v"(x));
-    return x;
-  };
   const auto stage = [&](int tile, const Codes<COLS>& x, int buf) {
     const int gi = (tile * kGroups + my_group) & 63;
     const float ks = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), gi));
@@ -228,8 +242,8 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
     }
   };
 
-  // Operands come from the LDS four products ahead.
-  constexpr int kAhead = 4;
+  // Operands come from the LDS four products ahead; where an operand has three, six.
+  constexpr int kAhead = TERMS == 3 ? 2 : 4;
   const auto k_operand = [&](uint32_t kr, int buf, int e) {  // product e = c * kTok32 + b of the scores
     const int b = e % kTok32, c = e / kTok32;
     return *reinterpret_cast<const u32x4*>(&lds.k[buf][(kr ^ (c << 5)) + b * 32 * D * 2]);
@@ -243,6 +257,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   // The tile's scores, of this wave's half of d; leaves the first operands of V in f.
   const auto scores = [&](f32x16 (&sc)[kTok32], u32x4 (&f)[kAhead], int buf) {
     const uint32_t kr = fresh(k_read), vr = fresh(v_read);
+    const uint32_t qr = kKept < DH / 16 ? fresh(q_place) : 0;
 #pragma unroll
     for (int b = 0; b < kTok32; ++b)
 #pragma unroll
@@ -254,8 +269,11 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       const bf16x8 k = __builtin_bit_cast(bf16x8, f[e % kAhead]);
       const int b = e % kTok32, c = e / kTok32;
 #pragma unroll
-      for (int w = TERMS - 1; w >= 0; --w)
-        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[c][w], sc[b], 0, 0, 0);
+      for (int w = TERMS - 1; w >= 0; --w) {
+        const bf16x8 qw = c < kKept ? q[c < kKept ? c : 0][w]
+                                    : lds.q[qr + ((c - kKept) * TERMS + w) * 64];
+        sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qw, sc[b], 0, 0, 0);
+      }
       f[e % kAhead] = e + kAhead < kScoreOps ? k_operand(kr, buf, e + kAhead)
                                              : v_operand(vr, buf, e + kAhead - kScoreOps);
 
@@ -270,7 +288,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), g0 + s));
     };
     if (!seen) {
-      const int lo = see_lo - t - 4 * g, hi = see_hi - t - 4 * g;
+      const int lo = see_from() - t - 4 * g, hi = see_hi - t - 4 * g;
 #pragma unroll
       for (int b = 0; b < kTok32; ++b)
 #pragma unroll
@@ -364,22 +382,23 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   // they are taken out of the tile, since 0 * NaN would reach the other rows. (All waves come
   // here together.)
   const auto take_out = [&](int tile, int buf) {
+    const int tl = lane_anew(), tn = tl & 31, tg = tl >> 5, thread = anew(threadIdx.x);
     int odd = 0;
-    for (int x = threadIdx.x; x < T::kBytes / 16; x += 64 * kWaves) {
+    for (int x = thread; x < T::kBytes / 16; x += 64 * kWaves) {
       const u32x4 v = *reinterpret_cast<const u32x4*>(&lds.v[buf][16 * x]);
 #pragma unroll
       for (int k = 0; k < 4; ++k)
         odd |= (v[k] & 0x7F80u) == 0x7F80u || (v[k] & 0x7F800000u) == 0x7F800000u;
     }
     if (!__syncthreads_or(odd)) return;
-    const int t = begin + tile * TOK;
+    const int t = begin + tile * TOK, see_lo = see_from();
     const int g0 = (tile * kGroups) & 63;
 #pragma unroll 1
     for (int s = 0; s < kGroups; ++s) {
       u32x4 by;                                  // 1 where the row sees the token
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int tt = t + 16 * s + 8 * (k >> 1) + 4 * g + 2 * (k & 1);
+        const int tt = t + 16 * s + 8 * (k >> 1) + 4 * tg + 2 * (k & 1);
         const bool here = !((absent >> (g0 + s)) & 1);
         by[k] = (here && tt >= see_lo && tt < see_hi ? 0x3F80u : 0u) |
                 (here && tt + 1 >= see_lo && tt + 1 < see_hi ? 0x3F800000u : 0u);
@@ -387,7 +406,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
 #pragma unroll
       for (int j = 0; j < DH / 32; ++j) {
         const u32x4 v = *reinterpret_cast<const u32x4*>(
-            &lds.v[buf][T::v_at(half * DH + 32 * j + n, 2 * s + g)]);
+            &lds.v[buf][T::v_at(half * DH + 32 * j + tn, 2 * s + tg)]);
         u32x4 is;                                // 1 where the value is not finite
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -404,7 +423,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       }
     }
     __syncthreads();
-    for (int x = threadIdx.x; x < T::kBytes / 16; x += 64 * kWaves) {
+    for (int x = thread; x < T::kBytes / 16; x += 64 * kWaves) {
       u32x4* at = reinterpret_cast<u32x4*>(&lds.v[buf][16 * x]);
       u32x4 v = *at;
 #pragma unroll
@@ -480,25 +499,28 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   }
 
   // results: the lane's columns 32 j + 8 b + 4 g + (0 .. 3) of row n
+  // (the lane's and the wave's numbers anew: no registers are kept for them through the tiles)
   l = lane_sum<32>(l);
+  const int el = lane_anew(), en = el & 31, eg = el >> 5;
+  const int ew = my_group + col0 / COLS * kGroups, end_half = ew / kRowWaves;
+  const int end_row = ew % kRowWaves * kWaveRows + en;
   if (live) {
-    const RowPlace place = row_place(a, it, h, rho);
+    const RowPlace place = row_place(a, it, h, it.tile * kManyRows + end_row);
     const Part<kManyRows, D> part = part_of<kManyRows, D>(a, it, h, item);
-    const int row = row_wave * kWaveRows + n;
 #pragma unroll
     for (int j = 0; j < DH / 32; ++j)
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         const f32x4 y = {acc[j][4 * b], acc[j][4 * b + 1], acc[j][4 * b + 2], acc[j][4 * b + 3]};
-        const int col = half * DH + 32 * j + 8 * b + 4 * g;
+        const int col = end_half * DH + 32 * j + 8 * b + 4 * eg;
         if (it.splits == 1) put_quad<ES>(a, place, col, y, l);
-        else part.put_quad(row, col / 4, y);
+        else part.put_quad(end_row, col / 4, y);
       }
-    if (g == 0 && half == 0) {
+    if (eg == 0 && end_half == 0) {
       if (it.splits == 1) {
         put_lse(a, place, ref == kNone ? 0.f : ref, l);
       } else {
-        part.put_stat(0, row, ref, l);
+        part.put_stat(0, end_row, ref, l);
       }
     }
   }
@@ -512,8 +534,8 @@ template <int TERMS, int D, int TOK, int HALVES>
 __global__ __launch_bounds__(64 * kRowWaves * HALVES, 2) void qcache_any_rows_kernel(
     QAttention a, uint32_t many) {
   __shared__ union Shared {
-    ManyShared<D, TOK, HALVES> many;
-    FewShared<D, kRowWaves * HALVES> few;
+    ManyShared<TERMS, D, TOK, HALVES> many;
+    FewShared<TERMS, D, kRowWaves * HALVES> few;
   } lds;
   if (blockIdx.x < many) many_rows_item<TERMS, D, TOK, HALVES>(a, blockIdx.x, lds.many);
   else few_rows_span<TERMS, D, kRowWaves * HALVES>(a, blockIdx.x - many, lds.few);
