@@ -501,7 +501,7 @@ int32_t cm_paged_workspace_size(const cm_pagedset* set, size_t* bytes_out);
  * mantissa bits, no infinity); page p of layer l's K is the [H][B][d] block at byte
  * (2l * P + p) * H * B * d, its V at ((2l + 1) * P + p) * H * B * d: the layout of
  * cm_pagedset's pool. scales_dev: [L][2][P][H] fp32, one for the B tokens of a page
- * and a head. A stored value is code * scale. d is 64, 128 or 256; B is 16, 32, 64
+ * and a head, not negative. A stored value is code * scale. d is 64, 128 or 256; B is 16, 32, 64
  * or 128; codes_dev is 16-byte, scales_dev 4-byte aligned.
  * A token's slot is page * B + its row in the page. */
 #define CM_QCACHE_MAX_REQUESTS 1024
@@ -619,7 +619,7 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
  * for one kernel name ("hash_prep", "hash_leaf", "hash_parent", "hash_final",
  * "knorm_rows", "knorm_tree", "order", "key_mask", "render_prep", "render",
  * "render_hash", "paged", "paged_hash_render", "qcache_tables", "qcache_write",
- * "qcache_attention", "qcache_join"). "hash_parent" is the trees above the
+ * "qcache_attention"). "hash_parent" is the trees above the
  * stripes that the chunk kernels fold, with the Ids where one launch makes both and
  * where tensors of 2 to 64 chunks leave only the Ids to make; "hash_final" the Ids
  * otherwise. "key_mask" includes the comparison of re-deliveries. */

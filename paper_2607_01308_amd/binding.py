@@ -298,7 +298,7 @@ def timing_query(kernel: str):
 
 KERNELS = ("hash_prep", "hash_leaf", "hash_parent", "hash_final", "knorm_rows", "knorm_tree",
            "order", "key_mask", "render_prep", "render", "render_hash", "paged",
-           "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention", "qcache_join")
+           "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention")
 
 
 class PagedSet:

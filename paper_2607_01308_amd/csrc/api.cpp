@@ -142,7 +142,7 @@ int64_t min_T(const cm::SetDesc& s) {
 const char* const kKernelNames[cm::K_COUNT] = {
     "hash_prep", "hash_leaf", "hash_parent", "hash_final", "knorm_rows", "knorm_tree",
     "order",     "key_mask",  "render_prep", "render",     "render_hash", "paged",
-    "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention", "qcache_join"};
+    "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention"};
 std::atomic<bool> g_timing{false};
 // set while this thread captures a call into a graph: no timing events then
 thread_local bool t_capturing = false;

@@ -325,7 +325,6 @@ enum KernelId {
   K_QCACHE_TABLES,
   K_QCACHE_WRITE,
   K_QCACHE_ATTENTION,
-  K_QCACHE_JOIN,
   K_COUNT
 };
 

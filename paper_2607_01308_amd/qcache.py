@@ -1,5 +1,5 @@
 """Serving a merged cache from 8-bit pages: the binding of cm_qcache_tables,
-cm_qcache_write and cm_qcache_attention (include/cmerge.h), and ServingCache, which
+cm_qcache_write and cm_qcache_attention (include/cmerge.h). ServingCache (serving.py)
 strings them together for a set of requests.
 
 A cache holds, for each layer and K/V, pages of B tokens of every head: codes

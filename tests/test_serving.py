@@ -1,0 +1,73 @@
+"""ServingCache's own bookkeeping, on the CPU: the library's tables are the plain ones
+(tests/qcache_ref.py), the cache is a stand-in."""
+
+import numpy as np
+import pytest
+import torch
+
+import qcache_ref as ref
+from paper_2607_01308_amd import serving
+from paper_2607_01308_amd.qcache import QCacheStep
+
+
+class FakeCache:
+    def __init__(self, P, B, L=2, H=2, d=64):
+        self.P, self.B, self.L, self.H, self.d = P, B, L, H, d
+        self.device = torch.device("cpu")
+
+
+@pytest.fixture
+def plain(monkeypatch):
+    """qcache_tables on the CPU; the calls it got."""
+    calls = []
+
+    def tables(pages, block, held, new, free, table, tokens, stream=None):
+        got = ref.tables(pages, block, held.tolist(), new.tolist(), free.tolist(), table.numpy())
+        assert got is not None and sum(new.tolist()) == tokens
+        table.copy_(torch.from_numpy(got[0]))
+        calls.append((held.clone(), new.clone(), got[4]))
+        return QCacheStep(torch.tensor(got[1], dtype=torch.int64),
+                          torch.tensor(got[2], dtype=torch.int32),
+                          torch.tensor(got[3], dtype=torch.int32),
+                          torch.tensor([0, tokens, got[4], max(got[3])]))
+
+    monkeypatch.setattr(serving, "qcache_tables", tables)
+    return calls
+
+
+@pytest.mark.parametrize("seed,P,B,places", [(0, 40, 16, 4), (1, 7, 32, 3), (2, 200, 16, 9), (3, 1, 16, 1)])
+def test_pages_are_dealt_once(plain, seed, P, B, places):
+    rng = np.random.default_rng(seed)
+    sc = serving.ServingCache(FakeCache(P, B), places, P * B)
+    for _ in range(300):
+        if rng.random() < 0.3:
+            sc.release(int(rng.integers(places)))
+        else:
+            new = [int(rng.integers(0, 3 * B)) if rng.random() < 0.5 else 0 for _ in range(places)]
+            before = (list(sc.lengths), sc.free_pages, sc.table.clone())
+            try:
+                step = sc.extend(new)
+            except (RuntimeError, ValueError):
+                assert before[:2] == (sc.lengths, sc.free_pages)
+                assert torch.equal(before[2], sc.table)
+                continue
+            assert plain[-1][0].tolist() == before[0] and plain[-1][1].tolist() == new
+            assert before[1] - sc.free_pages == plain[-1][2]
+            assert (step.tokens, step.max_rows) == (sum(new), max(new))
+        used = [int(p) for r in range(places) for p in sc.table[r, :-(-sc.lengths[r] // B)]]
+        free = sc._free[sc._head:sc._tail].tolist()
+        assert sorted(used + free) == list(range(P))
+        assert sc._held.tolist() == sc.lengths
+
+
+def test_layers_of_one_buffer():
+    one = torch.arange(3 * 2 * 2 * 10 * 4.).view(3, 2, 1, 2, 10, 4)
+    ks = [one[l, 0, :, :, :7] for l in range(3)]
+    got = serving._one_buffer(ks)
+    assert got is not None
+    assert torch.equal(got, torch.stack([k[0].transpose(0, 1) for k in ks]))
+    assert serving._one_buffer([k.clone() for k in ks]) is None
+    assert serving._one_buffer([ks[0], ks[2], ks[1]]) is None
+    assert serving._one_buffer([ks[0], ks[1], ks[1]]) is None
+    assert serving._one_buffer([ks[0]]) is not None
+    assert serving._one_buffer([ks[0], one[1, 0, :, :, :7].double()]) is None
