@@ -87,9 +87,11 @@ struct FindShared {
 // The workgroup's item from the lengths: every request's context is cut into equal ranges of
 // whole units so that about `items` ranges come out for all row tiles. Every workgroup looks
 // at all n <= 1024 lengths, a few a thread: two prefix sums, about 2 us, beside which other
-// workgroups stream (a plan made once would be a launch of its own, 5 us and more).
+// workgroups stream (a plan made once would be a launch of its own, 5 us and more). The grid and
+// the workspace hold `most` items, enough for requests that share no rows; where rows_dev lays
+// requests over one another so that more come out, no workgroup has an item.
 template <int ROWS, int THREADS>
-__device__ __forceinline__ Item find_item(const QAttention& a, int items, int item,
+__device__ __forceinline__ Item find_item(const QAttention& a, int items, int most, int item,
                                           FindShared& lds) {
   constexpr int kPer = CM_QCACHE_MAX_REQUESTS / THREADS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -130,6 +132,7 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int it
   const float want = cost / aim * 1.0001f;
   const int chunk = !a.split || want > 1e9f ? 1 << 30 : want > 1.f ? (int)want + 1 : 1;
   int splits[kPer], mine = 0;
+  if (all > (float)most) return Item{};          // (their number might not fit an int)
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     splits[k] = (int)((uint32_t)(units[k] + chunk - 1) / (uint32_t)chunk);
@@ -139,9 +142,13 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int it
   const int upto = wave_scan(mine);
   if (lane == 63) lds.items[wave] = upto;
   __syncthreads();
-  int at = upto - mine;
-  for (int w = 0; w < wave; ++w) at += lds.items[w];
-  if (item >= at && item < at + mine) {
+  int at = upto - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    if (w < wave) at += lds.items[w];
+    total += lds.items[w];
+  }
+  if (total <= most && item >= at && item < at + mine) {
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int here = tiles[k] * splits[k];

@@ -96,7 +96,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const int row_wave = wave % kRowWaves, half = wave / kRowWaves;
   const HeadItem hi = head_item(a.H, block);
   const int h = hi.h, item = hi.item;
-  const Item it = find_item<kManyRows, 64 * kWaves>(a, a.many_items, item, lds.find);
+  const Item it = find_item<kManyRows, 64 * kWaves>(a, a.many_items, a.many_max, item, lds.find);
   if (!it.any) return;
 
   // the lane's query row
