@@ -1416,7 +1416,6 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
   a.few_part = reinterpret_cast<float*>(ws + plan.few_at);
   a.many_part = reinterpret_cast<float*>(ws + plan.many_at);
   a.few_count = reinterpret_cast<int32_t*>(ws);
-  a.many_count = a.few_count + 2 * (int64_t)plan.few_max * c.H;
   a.split = plan.split;
   hipError_t e = cm::launch_qcache_attention(a, c.d, step->dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_attention");

@@ -44,14 +44,13 @@ struct QAttention {
   int32_t negate;     // the softmax scale is negative
   // For requests of few query rows and of many: the spans (few) or items (many) that their
   // contexts are cut into for each KV head, places of partial results for each KV head,
-  // where they are, [H][max], and their counters, [H][max][2].
+  // where they are, [H][max], and the counters of those for few, [H][max][2].
   int32_t few_items, few_max, many_items, many_max;
   float* few_part;
   float* many_part;
   int32_t* few_count;
-  int32_t* many_count;
   int32_t few_unit;   // tokens by which few rows' contexts are cut
-  int32_t split;      // 0: no request is cut
+  int32_t split;      // 0: no request of many rows is cut
 };
 
 hipError_t launch_qcache_tables(int64_t pages, int32_t b_shift, int32_t n, const int32_t* held,
@@ -64,7 +63,8 @@ hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t
 
 // Work items of an attention call: the split that fills the GPU and the bound that
 // sizes its grid and its workspace, from what the host knows.
-constexpr int64_t kCounters = 1 << 17;  // at the start of the workspace
+constexpr int64_t kCounters = 1 << 17;  // at the start of the workspace; 4 H or 2048 are used
+constexpr int64_t kMostSplit = 1 << 16;  // items of many rows, beyond which none is cut
 struct QAttentionPlan {
   int32_t few_unit, few_items, few_max, many_items, many_max;
   bool split;

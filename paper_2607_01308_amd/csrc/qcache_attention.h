@@ -321,13 +321,13 @@ __device__ __forceinline__ void get_part(const float* at, float& x, float& y) {
   y = __uint_as_float(w[1]);
 }
 
-// Partial results of an item: `rows` rows of D values, then the exponent m and the sum l of
-// each row: of the item, and of the group that it is the first of. The values are stored as
-// the lanes hold them, two columns of one row after another: a store of a wave fills whole
-// lines (row after row it was 8 bytes of 64 lines, which such stores write one by one).
-template <int ROWS, int D>
+// Partial results of a segment of few rows: `rows` rows of D values, then the exponent m and the
+// sum l of each row: of the segment, and of the group that it is the first of. The values are
+// stored as the lanes hold them, two columns of one row after another: a store of a wave fills
+// whole lines (row after row it was 8 bytes of 64 lines, which such stores write one by one).
+template <int D>
 struct Part {
-  static constexpr int64_t kFloats = (int64_t)ROWS * (D + 4);
+  static constexpr int64_t kFloats = (int64_t)kFewRows * (D + 4);
   float* at;
   int rows;
   __device__ __forceinline__ void put_quad(int row, int q, f32x4 v) const {
@@ -343,20 +343,15 @@ struct Part {
     return f32x4{x[0], x[1], x[2], x[3]};
   }
   __device__ __forceinline__ void put_stat(int level, int row, float m, float l) const {
-    put_part(at + ROWS * D + 2 * (ROWS * level + row), m, l);
+    put_part(at + kFewRows * D + 2 * (kFewRows * level + row), m, l);
   }
   __device__ __forceinline__ void stat(int level, int row, float& m, float& l) const {
-    get_part(at + ROWS * D + 2 * (ROWS * level + row), m, l);
+    get_part(at + kFewRows * D + 2 * (kFewRows * level + row), m, l);
   }
 };
-template <int ROWS, int D>
-__device__ __forceinline__ Part<ROWS, D> part_of(const QAttention& a, const Item& it, int h,
-                                                 int place) {
-  constexpr bool kFew = ROWS == kFewRows;
-  const int rows = it.count * a.G - it.tile * ROWS;
-  return {(kFew ? a.few_part : a.many_part) +
-              ((int64_t)h * (kFew ? a.few_max : a.many_max) + place) * Part<ROWS, D>::kFloats,
-          rows < ROWS ? rows : ROWS};
+template <int D>
+__device__ __forceinline__ Part<D> part_of(const QAttention& a, const Item& it, int h, int place) {
+  return {a.few_part + ((int64_t)h * a.few_max + place) * Part<D>::kFloats, it.count * a.G};
 }
 
 // x, of which the compiler does not know that it is x: what is computed from it is computed where
@@ -377,9 +372,15 @@ __device__ __forceinline__ int lane_anew() {
 struct Joined {
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   float m = kNone, l = 0.f;
+  // the first `there` of N results
   template <int N>
-  __device__ __forceinline__ void add(const f32x4 (&x)[N], const float (&xm)[N],
-                                      const float (&xl)[N]) {
+  __device__ __forceinline__ void add(f32x4 (&x)[N], float (&xm)[N], float (&xl)[N], int there) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {                // (what is not there weighs nothing)
+      x[k] = k < there ? x[k] : f32x4{0.f, 0.f, 0.f, 0.f};
+      xm[k] = k < there ? xm[k] : kNone;
+      xl[k] = k < there ? xl[k] : 0.f;
+    }
     float top = m;
 #pragma unroll
     for (int k = 0; k < N; ++k) top = fmaxf(top, xm[k]);
@@ -402,11 +403,11 @@ struct Joined {
 // Joins `count` partial results, in the places slot(0), slot(1), ..: into the output (`whole`)
 // or, as the result of a group, into the first of them. In order, by all threads, each
 // several quads of columns at a time where there are few results to load for each.
-template <int ROWS, int D, int ES, int THREADS, int BATCH, int QUADS, class Slot>
+template <int D, int ES, int THREADS, int BATCH, int QUADS, class Slot>
 __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, int h, int count,
                                           int level, bool whole, Slot slot) {
   constexpr int kQuads = D / 4;
-  const Part<ROWS, D> p0 = part_of<ROWS, D>(a, it, h, slot(0));
+  const Part<D> p0 = part_of<D>(a, it, h, slot(0));
   const int total = p0.rows * kQuads;
   for (int x0 = anew(threadIdx.x); x0 < total; x0 += THREADS * QUADS) {
     Joined sum[QUADS];
@@ -415,7 +416,7 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
       float m[QUADS][BATCH], l[QUADS][BATCH];
 #pragma unroll
       for (int k = 0; k < BATCH; ++k) {
-        const Part<ROWS, D> p = part_of<ROWS, D>(a, it, h, slot(s + k < count ? s + k : s));
+        const Part<D> p = part_of<D>(a, it, h, slot(s + k < count ? s + k : s));
 #pragma unroll
         for (int u = 0; u < QUADS; ++u) {
           const int x = x0 + u * THREADS < total ? x0 + u * THREADS : x0;
@@ -425,16 +426,7 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
         }
       }
 #pragma unroll
-      for (int u = 0; u < QUADS; ++u) {
-#pragma unroll
-        for (int k = 0; k < BATCH; ++k) {
-          const bool there = s + k < count;      // (what is not there weighs nothing)
-          o[u][k] = there ? o[u][k] : f32x4{0.f, 0.f, 0.f, 0.f};
-          m[u][k] = there ? m[u][k] : kNone;
-          l[u][k] = there ? l[u][k] : 0.f;
-        }
-        sum[u].add(o[u], m[u], l[u]);
-      }
+      for (int u = 0; u < QUADS; ++u) sum[u].add(o[u], m[u], l[u], count - s);
     }
 #pragma unroll
     for (int u = 0; u < QUADS; ++u) {
@@ -442,7 +434,7 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
       if (x >= total) break;
       const int quad = (int)((uint32_t)x / (uint32_t)p0.rows), row = x - quad * p0.rows;
       if (whole) {
-        const RowPlace place = row_place(a, it, h, it.tile * ROWS + row);
+        const RowPlace place = row_place(a, it, h, row);
         put_quad<ES>(a, place, 4 * quad, sum[u].o, sum[u].l);
         if (quad == 0) put_lse(a, place, sum[u].m == kNone ? 0.f : sum[u].m, sum[u].l);
       } else {
@@ -453,11 +445,11 @@ __device__ __forceinline__ void join_some(const QAttention& a, const Item& it, i
   }
 }
 constexpr int kJoin = 16;   // partial results joined at a time
-template <int ROWS, int D, int ES, int THREADS, class Slot>
+template <int D, int ES, int THREADS, class Slot>
 __device__ __forceinline__ void join_parts(const QAttention& a, const Item& it, int h, int count,
                                            int level, bool whole, Slot slot) {
-  if (count <= 4) join_some<ROWS, D, ES, THREADS, 4, 4>(a, it, h, count, level, whole, slot);
-  else join_some<ROWS, D, ES, THREADS, 8, 2>(a, it, h, count, level, whole, slot);
+  if (count <= 4) join_some<D, ES, THREADS, 4, 4>(a, it, h, count, level, whole, slot);
+  else join_some<D, ES, THREADS, 8, 2>(a, it, h, count, level, whole, slot);
 }
 
 // Whether this workgroup is the last of `count` to come to a counter, which the last one
@@ -483,22 +475,20 @@ __device__ __forceinline__ bool last_to_come(int32_t* counter, int count, int* s
 // every kJoin of them (more where there are more than kJoin^2) joins these, the last of the
 // groups joins the groups. Which workgroup comes last changes nothing: the order of the sums is
 // that of the ranges. slot(i) is the place of result i; a place has two counters.
-template <int ROWS, int D, int ES, int THREADS, class Slot>
+template <int D, int ES, int THREADS, class Slot>
 __device__ __forceinline__ void finish_split(const QAttention& a, const Item& it, int h, int split,
                                              int splits, int* s_flag, Slot slot) {
-  constexpr bool kFew = ROWS == kFewRows;
-  int32_t* counters =
-      (kFew ? a.few_count : a.many_count) + 2 * (int64_t)h * (kFew ? a.few_max : a.many_max);
+  int32_t* counters = a.few_count + 2 * (int64_t)h * a.few_max;
   int size = kJoin;
   while (size * size < splits) size += kJoin;
   const int group = split / size, groups = (splits + size - 1) / size;
   const int here = group * size, members = splits - here < size ? splits - here : size;
   if (!last_to_come(counters + 2 * slot(here), members, s_flag)) return;
-  join_parts<ROWS, D, ES, THREADS>(a, it, h, members, 0, groups == 1,
-                                   [&](int i) { return slot(here + i); });
+  join_parts<D, ES, THREADS>(a, it, h, members, 0, groups == 1,
+                             [&](int i) { return slot(here + i); });
   if (groups == 1) return;
   if (!last_to_come(counters + 2 * slot(0) + 1, groups, s_flag)) return;
-  join_parts<ROWS, D, ES, THREADS>(a, it, h, groups, 1, true, [&](int i) { return slot(i * size); });
+  join_parts<D, ES, THREADS>(a, it, h, groups, 1, true, [&](int i) { return slot(i * size); });
 }
 
 template <int TERMS, int D>

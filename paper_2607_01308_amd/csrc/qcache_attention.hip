@@ -36,10 +36,11 @@ QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n,
   p.few_max = 2 * p.few_items;                       // a span's first and last segment
   // a request's ranges round up once
   p.many_max = many ? (int32_t)((rows + kManyRows - 1) / kManyRows + n + p.many_items) : 0;
-  p.split = 2 * ((int64_t)p.few_max + p.many_max) * H <= kCounters;
+  // (so many row tiles fill the GPU as they are; their partial results would be gigabytes)
+  p.split = (int64_t)p.many_max * H <= kMostSplit;
   const size_t row = sizeof(float) * (size_t)(d + 4) * (size_t)H;
   p.few_at = sizeof(int32_t) * kCounters;
-  p.many_at = p.few_at + (p.split ? align_up(row * kFewRows * (size_t)p.few_max, kWsAlign) : 0);
+  p.many_at = p.few_at + align_up(row * kFewRows * (size_t)p.few_max, kWsAlign);
   p.bytes = p.many_at + (p.split ? row * kManyRows * (size_t)p.many_max : 0);
   return p;
 }

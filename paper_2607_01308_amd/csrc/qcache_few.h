@@ -344,7 +344,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
     __syncthreads();
   }
   if (wave == 0 && live) {
-    const Part<kFewRows, D> part = part_of<kFewRows, D>(a, it, h, slot);
+    const Part<D> part = part_of<D>(a, it, h, slot);
     const RowPlace place = row_place(a, it, h, it.tile * kFewRows + en);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -397,9 +397,8 @@ __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
     total += lds.sums[v];
   }
   total = __builtin_amdgcn_readfirstlane(total);
-  const int span = a.split ? (total + a.few_items - 1) / a.few_items : 0;
-  // (without splits a workgroup takes the requests w, w + few_items, ..)
-  int u = a.split ? w * span : 0;
+  const int span = (total + a.few_items - 1) / a.few_items;
+  int u = w * span;
   const int stop = u + span < total ? u + span : total;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
@@ -412,7 +411,7 @@ __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
   }
   if (threadIdx.x == 0) lds.pos[a.n] = total;
   __syncthreads();
-  if (a.split && u >= total) return;
+  if (u >= total) return;
 
   Item it;
   it.tile = 0;
@@ -422,35 +421,28 @@ __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
     it.r = r;
     it.begin = visible_begin(a, it.count, it.len);
   };
-  // (with spans: request after request until the span's end; without: every few_items-th)
-  int r = a.split ? __builtin_amdgcn_readfirstlane(lds.first) : w;
-  while (a.split ? u < stop : r < a.n) {
+  int r = __builtin_amdgcn_readfirstlane(lds.first);
+  while (u < stop) {
     const int from = __builtin_amdgcn_readfirstlane(lds.pos[r]);
     const int to = __builtin_amdgcn_readfirstlane(lds.pos[r + 1]);
     if (from != to) {
       look(r);
-      it.splits = 1;
-      it.chunk = it.len - it.begin;
-      int part = 0, first = 0;
-      if (a.split) {
-        const int upto_u = to < stop ? to : stop;
-        it.begin += (u - from) * a.few_unit;
-        it.chunk = (upto_u - u) * a.few_unit;
-        u = upto_u;
-        // the spans that hold some of it
-        first = from / span;
-        part = w - first;
-        it.splits = (to - 1) / span - first + 1;
-      }
+      const int upto_u = to < stop ? to : stop;
+      it.begin += (u - from) * a.few_unit;
+      it.chunk = (upto_u - u) * a.few_unit;
+      u = upto_u;
+      // the spans that hold some of it
+      const int first = from / span, part = w - first;
+      it.splits = (to - 1) / span - first + 1;
       // (in the first of them another request may come before it)
       const auto slot = [&](int i) {
         return i == 0 ? 2 * first + (from > first * span ? 1 : 0) : 2 * (first + i);
       };
       few_rows_segment<TERMS, D, WAVES>(a, it, h, slot(part), lds);
       if (it.splits > 1)
-        finish_split<kFewRows, D, ES, kThreads>(a, it, h, part, it.splits, &lds.flag, slot);
+        finish_split<D, ES, kThreads>(a, it, h, part, it.splits, &lds.flag, slot);
     }
-    r += a.split ? 1 : a.few_items;
+    ++r;
   }
 }
 

@@ -74,8 +74,30 @@ struct ManyShared {
   static constexpr int kQuery = shared_chunks(TERMS, D / HALVES) * TERMS;
   bf16x8 q[kQuery ? kRowWaves * HALVES * kQuery * 64 : 1];  // [wave][chunk][term][lane]
   FindShared find;
-  int flag;
 };
+
+// Partial results of an item: quads of columns, each of the tile's rows one after another, then
+// the exponent m and the sum l of each row. The join is a launch of its own, so they are stored
+// and loaded like any other data.
+template <int D>
+struct ManyPart {
+  static constexpr int64_t kFloats = (int64_t)kManyRows * (D + 4);
+  float* at;
+  int rows;
+  __device__ __forceinline__ f32x4* quad(int row, int q) const {
+    return reinterpret_cast<f32x4*>(at) + q * rows + row;
+  }
+  __device__ __forceinline__ f32x2v* stat(int row) const {
+    return reinterpret_cast<f32x2v*>(at + kManyRows * D) + row;
+  }
+};
+template <int D>
+__device__ __forceinline__ ManyPart<D> many_part(const QAttention& a, const Item& it, int h,
+                                                 int place) {
+  const int rows = it.count * a.G - it.tile * kManyRows;
+  return {a.many_part + ((int64_t)h * a.many_max + place) * ManyPart<D>::kFloats,
+          rows < kManyRows ? rows : kManyRows};
+}
 
 // HALVES 2: two waves share 32 rows, each half of d: half of the sum of a score, which
 // they exchange through the LDS, and half of the output's columns.
@@ -506,7 +528,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const int end_row = ew % kRowWaves * kWaveRows + en;
   if (live) {
     const RowPlace place = row_place(a, it, h, it.tile * kManyRows + end_row);
-    const Part<kManyRows, D> part = part_of<kManyRows, D>(a, it, h, item);
+    const ManyPart<D> part = many_part<D>(a, it, h, item);
 #pragma unroll
     for (int j = 0; j < DH / 32; ++j)
 #pragma unroll
@@ -514,19 +536,16 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
         const f32x4 y = {acc[j][4 * b], acc[j][4 * b + 1], acc[j][4 * b + 2], acc[j][4 * b + 3]};
         const int col = end_half * DH + 32 * j + 8 * b + 4 * eg;
         if (it.splits == 1) put_quad<ES>(a, place, col, y, l);
-        else part.put_quad(end_row, col / 4, y);
+        else *part.quad(end_row, col / 4) = y;
       }
     if (eg == 0 && end_half == 0) {
       if (it.splits == 1) {
         put_lse(a, place, ref == kNone ? 0.f : ref, l);
       } else {
-        part.put_stat(0, end_row, ref, l);
+        *part.stat(end_row) = f32x2v{ref, l};
       }
     }
   }
-  if (it.splits > 1)
-    finish_split<kManyRows, D, ES, 64 * kWaves>(a, it, h, it.split, it.splits, &lds.flag,
-                                                [&](int i) { return item - it.split + i; });
 }
 
 // Requests of many rows in the first `many` workgroups, of few in the others.
@@ -541,6 +560,49 @@ __global__ __launch_bounds__(64 * kRowWaves * HALVES, 2) void qcache_any_rows_ke
   else few_rows_span<TERMS, D, kRowWaves * HALVES>(a, blockIdx.x - many, lds.few);
 }
 
+// Joins the partial results of the tiles whose context is cut: of the s workgroups of a tile's
+// items each takes an s-th of its quads of columns, over all s results, in their order. (Joined
+// by the last of the tile's workgroups in the launch before, 16 questions of 84 rows of d = 256
+// kept 32 of the 256 compute units busy while 18 MB came back: 97 us for the call, not 73.)
+// THREADS: those of the launch before, so that find_item makes the same sums.
+template <int D, int ES, int THREADS>
+__global__ __launch_bounds__(THREADS) void qcache_join_kernel(QAttention a) {
+  __shared__ FindShared find;
+  const HeadItem hi = head_item(a.H, blockIdx.x);
+  const Item it = find_item<kManyRows, THREADS>(a, a.many_items, a.many_max, hi.item, find);
+  if (!it.any || it.splits == 1) return;
+  const ManyPart<D> p0 = many_part<D>(a, it, hi.h, hi.item - it.split);
+  const int total = p0.rows * (D / 4);
+  const int share = (total + it.splits - 1) / it.splits;
+  const int begin = it.split * share, end = begin + share < total ? begin + share : total;
+  const auto join = [&](auto batch) {
+    constexpr int BATCH = decltype(batch)::value;
+    for (int x = begin + (int)threadIdx.x; x < end; x += THREADS) {
+      const int quad = (int)((uint32_t)x / (uint32_t)p0.rows), row = x - quad * p0.rows;
+      Joined sum;
+      for (int s = 0; s < it.splits; s += BATCH) {
+        f32x4 o[BATCH];
+        float m[BATCH], l[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+          ManyPart<D> p = p0;
+          p.at += (int64_t)(s + k < it.splits ? s + k : s) * ManyPart<D>::kFloats;
+          o[k] = *p.quad(row, quad);
+          const f32x2v st = *p.stat(row);
+          m[k] = st[0];
+          l[k] = st[1];
+        }
+        sum.add(o, m, l, it.splits - s);
+      }
+      const RowPlace place = row_place(a, it, hi.h, it.tile * kManyRows + row);
+      put_quad<ES>(a, place, 4 * quad, sum.o, sum.l);
+      if (quad == 0) put_lse(a, place, sum.m == kNone ? 0.f : sum.m, sum.l);
+    }
+  };
+  if (it.splits <= 4) join(std::integral_constant<int, 4>{});
+  else join(std::integral_constant<int, 16>{});
+}
+
 }  // namespace
 
 template <int TERMS, int D>
@@ -550,6 +612,10 @@ hipError_t launch_qcache_any_rows(const QAttention& a, uint32_t many, uint32_t f
   constexpr int HALVES = many_halves(D, TERMS);
   hipLaunchKernelGGL((qcache_any_rows_kernel<TERMS, D, TOK, HALVES>), dim3(many + few),
                      dim3(64 * kRowWaves * HALVES), 0, stream, a, many);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !a.split) return e;
+  hipLaunchKernelGGL((qcache_join_kernel<D, TERMS == 1 ? 2 : 4, 64 * kRowWaves * HALVES>),
+                     dim3(many), dim3(64 * kRowWaves * HALVES), 0, stream, a);
   return hipGetLastError();
 }
 
