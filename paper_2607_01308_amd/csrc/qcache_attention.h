@@ -14,10 +14,15 @@ constexpr int kManyRows = 128;  // and of the kernel for many
 // other, whole.
 __host__ __device__ __forceinline__ bool few_rows(int64_t rows) { return rows <= kFewRows; }
 
-// Waves that share their rows in the kernel for many (qcache_prompt.hip): a wave's registers
-// hold its queries' terms, d * terms / 4 of them, and its columns of the output, d / 2; beyond
-// 96 two waves share.
-constexpr int many_halves(int d, int terms) { return d * (terms + 1) > 256 ? 2 : 1; }
+// Waves that share their rows in the kernel for many (qcache_prompt.hip). A wave's registers hold
+// its queries' terms, d * terms / 4 of them, and its columns of the output, d / 2. For d = 256 two
+// waves share (one wave for all columns and half as many waves: 4096 queries over 16384 tokens 3%
+// slower, short questions 10%).
+constexpr int many_halves(int d) { return d > 128 ? 2 : 1; }
+
+// Workgroups of that kernel on a compute unit. Three terms of d = 128 take the registers of two
+// waves (two waves that share rows instead: 1024 queries over 16384 tokens 948 us, so 797).
+constexpr int many_groups(int d, int terms) { return d * (terms + 1) > 256 ? 1 : 2; }
 
 struct Item {
   int32_t r, tile, split, splits;  // request, row tile, range of its context, how many

@@ -22,7 +22,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void qcache_few_rows_kernel(QAtt
 QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows,
                                      int32_t max_rows, int64_t longest, int32_t dtype) {
   QAttentionPlan p;
-  // workgroups that run together: two on a compute unit, or one of twice the waves
+  // workgroups that run together for few rows: two on a compute unit
   const int64_t groups = 2 * device_cu_count();
   const int32_t terms = dtype == CM_BF16 ? 1 : 3;
   const int64_t rows = n_rows * G;
@@ -32,7 +32,7 @@ QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n,
   p.few_unit = kUnit;
   while (n * (longest / p.few_unit + 1) > 0x7FFFFFFF) p.few_unit *= 2;
   p.few_items = per_head(groups);
-  p.many_items = per_head(groups / many_halves(d, terms));
+  p.many_items = per_head(device_cu_count() * many_groups(d, terms));
   p.few_max = 2 * p.few_items;                       // a span's first and last segment
   // a request's ranges round up once
   p.many_max = many ? (int32_t)((rows + kManyRows - 1) / kManyRows + n + p.many_items) : 0;

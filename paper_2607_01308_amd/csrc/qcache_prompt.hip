@@ -60,9 +60,11 @@ struct Codes {
   uint32_t v[COLS / 16];
 };
 
-// 16-column chunks of its queries that a wave keeps in the LDS: three terms of 128 columns
-// leave no registers for the last two.
-constexpr int shared_chunks(int terms, int columns) { return terms * columns > 256 ? 2 : 0; }
+// 16-column chunks of its queries that a wave keeps in the LDS: where two waves share a SIMD's
+// registers three terms of 128 columns leave none for the last two.
+constexpr int shared_chunks(int terms, int columns, int halves) {
+  return halves == 2 && terms * columns > 256 ? 2 : 0;
+}
 
 // The LDS of a workgroup.
 template <int TERMS, int D, int TOK, int HALVES>
@@ -71,7 +73,7 @@ struct ManyShared {
   uint8_t v[2][D * TOK * 2];
   // halves of scores that waves exchange
   f32x4 half[HALVES == 2 ? kRowWaves * HALVES * (TOK / 32) * 4 * 64 : 1];
-  static constexpr int kQuery = shared_chunks(TERMS, D / HALVES) * TERMS;
+  static constexpr int kQuery = shared_chunks(TERMS, D / HALVES, HALVES) * TERMS;
   bf16x8 q[kQuery ? kRowWaves * HALVES * kQuery * 64 : 1];  // [wave][chunk][term][lane]
   FindShared find;
 };
@@ -139,7 +141,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   end = end < sight.any_hi ? end : sight.any_hi;
   const int tiles = end > begin ? (end - begin + TOK - 1) / TOK : 0;
 
-  constexpr int kKept = DH / 16 - shared_chunks(TERMS, DH);
+  constexpr int kKept = DH / 16 - shared_chunks(TERMS, DH, HALVES);
   bf16x8 q[kKept][TERMS];
 #pragma unroll
   for (int c = 0; c < kKept; ++c)
@@ -550,7 +552,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
 
 // Requests of many rows in the first `many` workgroups, of few in the others.
 template <int TERMS, int D, int TOK, int HALVES>
-__global__ __launch_bounds__(64 * kRowWaves * HALVES, 2) void qcache_any_rows_kernel(
+__global__ __launch_bounds__(64 * kRowWaves * HALVES, many_groups(D, TERMS) * HALVES) void qcache_any_rows_kernel(
     QAttention a, uint32_t many) {
   __shared__ union Shared {
     ManyShared<TERMS, D, TOK, HALVES> many;
@@ -609,7 +611,7 @@ template <int TERMS, int D>
 hipError_t launch_qcache_any_rows(const QAttention& a, uint32_t many, uint32_t few,
                                   hipStream_t stream) {
   constexpr int TOK = D == 256 ? 32 : 64;
-  constexpr int HALVES = many_halves(D, TERMS);
+  constexpr int HALVES = many_halves(D);
   hipLaunchKernelGGL((qcache_any_rows_kernel<TERMS, D, TOK, HALVES>), dim3(many + few),
                      dim3(64 * kRowWaves * HALVES), 0, stream, a, many);
   const hipError_t e = hipGetLastError();
