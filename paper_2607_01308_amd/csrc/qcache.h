@@ -48,6 +48,7 @@ struct QAttention {
   int32_t few_items, few_max, many_items, many_max;
   float* few_part;
   float* many_part;
+  void* many_found;   // the items of many rows, [many_max]
   int32_t* few_count;
   int32_t few_unit;   // tokens by which few rows' contexts are cut
   int32_t split;      // 0: no request of many rows is cut
@@ -68,7 +69,7 @@ constexpr int64_t kMostSplit = 1 << 16;  // items of many rows, beyond which non
 struct QAttentionPlan {
   int32_t few_unit, few_items, few_max, many_items, many_max;
   bool split;
-  size_t few_at, many_at, bytes;  // partial results in the workspace, its size
+  size_t few_at, found_at, many_at, bytes;  // partial results in the workspace, its size
 };
 QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows,
                                      int32_t max_rows, int64_t longest, int32_t dtype);

@@ -40,7 +40,8 @@ QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n,
   p.split = (int64_t)p.many_max * H <= kMostSplit;
   const size_t row = sizeof(float) * (size_t)(d + 4) * (size_t)H;
   p.few_at = sizeof(int32_t) * kCounters;
-  p.many_at = p.few_at + align_up(row * kFewRows * (size_t)p.few_max, kWsAlign);
+  p.found_at = p.few_at + align_up(row * kFewRows * (size_t)p.few_max, kWsAlign);
+  p.many_at = p.found_at + align_up(p.split ? sizeof(Item) * (size_t)p.many_max : 0, kWsAlign);
   p.bytes = p.many_at + (p.split ? row * kManyRows * (size_t)p.many_max : 0);
   return p;
 }

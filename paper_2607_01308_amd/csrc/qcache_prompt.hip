@@ -121,6 +121,8 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const HeadItem hi = head_item(a.H, block);
   const int h = hi.h, item = hi.item;
   const Item it = find_item<kManyRows, 64 * kWaves>(a, a.many_items, a.many_max, item, lds.find);
+  if (a.split && h == 0 && item < a.many_max && threadIdx.x == 0)
+    reinterpret_cast<Item*>(a.many_found)[item] = it;
   if (!it.any) return;
 
   // the lane's query row
@@ -562,24 +564,26 @@ __global__ __launch_bounds__(64 * kRowWaves * HALVES, many_groups(D, TERMS) * HA
   else few_rows_span<TERMS, D, kRowWaves * HALVES>(a, blockIdx.x - many, lds.few);
 }
 
-// Joins the partial results of the tiles whose context is cut: of the s workgroups of a tile's
-// items each takes an s-th of its quads of columns, over all s results, in their order. (Joined
-// by the last of the tile's workgroups in the launch before, 16 questions of 84 rows of d = 256
-// kept 32 of the 256 compute units busy while 18 MB came back: 97 us for the call, not 73.)
-// THREADS: those of the launch before, so that find_item makes the same sums.
-template <int D, int ES, int THREADS>
-__global__ __launch_bounds__(THREADS) void qcache_join_kernel(QAttention a) {
-  __shared__ FindShared find;
+// Joins the partial results of the tiles whose context is cut: kJoinGroups workgroups for each of
+// a tile's s items take equal parts of its quads of columns, over all s results, in their order.
+// The items are those that the launch before has found. (Joined by the last of a tile's workgroups
+// in that launch, 16 questions of 84 rows of d = 256 kept 32 of the 256 compute units busy while
+// 18 MB came back, 40 us.)
+constexpr int kJoinGroups = 4, kJoinThreads = 256;
+template <int D, int ES>
+__global__ __launch_bounds__(kJoinThreads) void qcache_join_kernel(QAttention a) {
   const HeadItem hi = head_item(a.H, blockIdx.x);
-  const Item it = find_item<kManyRows, THREADS>(a, a.many_items, a.many_max, hi.item, find);
+  if (hi.item >= a.many_max) return;
+  const Item it = reinterpret_cast<const Item*>(a.many_found)[hi.item];
   if (!it.any || it.splits == 1) return;
   const ManyPart<D> p0 = many_part<D>(a, it, hi.h, hi.item - it.split);
   const int total = p0.rows * (D / 4);
-  const int share = (total + it.splits - 1) / it.splits;
-  const int begin = it.split * share, end = begin + share < total ? begin + share : total;
+  const int parts = it.splits * kJoinGroups, part = it.split * kJoinGroups + (int)blockIdx.y;
+  const int share = (total + parts - 1) / parts;
+  const int begin = part * share, end = begin + share < total ? begin + share : total;
   const auto join = [&](auto batch) {
     constexpr int BATCH = decltype(batch)::value;
-    for (int x = begin + (int)threadIdx.x; x < end; x += THREADS) {
+    for (int x = begin + (int)threadIdx.x; x < end; x += kJoinThreads) {
       const int quad = (int)((uint32_t)x / (uint32_t)p0.rows), row = x - quad * p0.rows;
       Joined sum;
       for (int s = 0; s < it.splits; s += BATCH) {
@@ -602,6 +606,7 @@ __global__ __launch_bounds__(THREADS) void qcache_join_kernel(QAttention a) {
     }
   };
   if (it.splits <= 4) join(std::integral_constant<int, 4>{});
+  else if (it.splits <= 8) join(std::integral_constant<int, 8>{});
   else join(std::integral_constant<int, 16>{});
 }
 
@@ -616,8 +621,8 @@ hipError_t launch_qcache_any_rows(const QAttention& a, uint32_t many, uint32_t f
                      dim3(64 * kRowWaves * HALVES), 0, stream, a, many);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.split) return e;
-  hipLaunchKernelGGL((qcache_join_kernel<D, TERMS == 1 ? 2 : 4, 64 * kRowWaves * HALVES>),
-                     dim3(many), dim3(64 * kRowWaves * HALVES), 0, stream, a);
+  hipLaunchKernelGGL((qcache_join_kernel<D, TERMS == 1 ? 2 : 4>), dim3(many, kJoinGroups),
+                     dim3(kJoinThreads), 0, stream, a);
   return hipGetLastError();
 }
 
