@@ -605,9 +605,11 @@ typedef struct {
 } cm_qattention;
 
 /* Workspace: cm_qcache_attention_size() bytes (n, n_rows, max_rows, table_width,
- * q_heads and the cache's shape decide it, not the lengths). It must be zero before its first use and used
- * for nothing else: a call counts in it which parts of the step are done, and leaves the
- * counters at zero. */
+ * q_heads and the cache's shape decide it, not the lengths), 256-byte aligned. Its first
+ * CM_QCACHE_COUNTER_BYTES must be zero before its first use, and it is used for nothing
+ * else: a call counts there which parts of the step are done, and leaves the counters at
+ * zero. Calls that may overlap have workspaces of their own. */
+#define CM_QCACHE_COUNTER_BYTES (1 << 19)
 int32_t cm_qcache_attention_size(const cm_qcache* cache, const cm_qattention* step,
                                  size_t* bytes_out);
 int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qattention* step,

@@ -16,6 +16,7 @@ CM_EDTYPE = -3
 CM_ENONFINITE = -4
 CM_EHIP = -5
 CM_EWORKSPACE = -6
+CM_QCACHE_COUNTER_BYTES = 1 << 19
 
 CM_F32 = 0
 CM_BF16 = 1

@@ -64,7 +64,8 @@ hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t
 
 // Work items of an attention call: the split that fills the GPU and the bound that
 // sizes its grid and its workspace, from what the host knows.
-constexpr int64_t kCounters = 1 << 17;  // at the start of the workspace; 4 H or 2048 are used
+// counters at the start of the workspace; 4 H or 2048 are used
+constexpr int64_t kCounters = CM_QCACHE_COUNTER_BYTES / (int64_t)sizeof(int32_t);
 constexpr int64_t kMostSplit = 1 << 16;  // items of many rows, beyond which none is cut
 struct QAttentionPlan {
   int32_t few_unit, few_items, few_max, many_items, many_max;

@@ -178,18 +178,30 @@ _WS: Dict[tuple, torch.Tensor] = {}
 
 def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
     """Scratch of the calls enqueued on a stream, cached for (device, stream) and
-    allocated there, so calls on two streams never share it."""
+    allocated there, so calls on two streams never share it. A call that is being captured
+    gets scratch of its graph's own memory, whose counters every replay clears: scratch that
+    is cached may be replaced by a larger one while the graph still refers to it."""
     need = ctypes.c_size_t(0)
     C.check(C.lib().cm_qcache_attention_size(ctypes.byref(cache.struct), ctypes.byref(step),
                                              ctypes.byref(need)), "cm_qcache_attention_size")
     key = (cache.device, s.cuda_stream)
     ws = _WS.get(key)
-    if ws is None or ws.numel() < need.value:
+    capturing = _capturing(s)
+    if capturing or ws is None or ws.numel() < need.value:
         with torch.cuda.stream(s):
-            # zero at first: the calls count in it, and leave their counters at zero
-            ws = torch.zeros(max(need.value, 256), dtype=torch.uint8, device=cache.device)
-        _WS[key] = ws
+            ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
+            # the calls count in it, and leave their counters at zero
+            ws[:C.CM_QCACHE_COUNTER_BYTES].zero_()
+        if not capturing:
+            _WS[key] = ws
     return ws
+
+
+def _capturing(s) -> bool:
+    if s.cuda_stream == torch.cuda.current_stream(s.device).cuda_stream:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(s):
+        return torch.cuda.is_current_stream_capturing()
 
 
 def release_qcache_workspace() -> None:
