@@ -176,17 +176,19 @@ def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
 _WS: Dict[tuple, torch.Tensor] = {}
 
 
-def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
-    """Scratch of the calls enqueued on a stream, cached for (device, stream) and
-    allocated there, so calls on two streams never share it. A call that is being captured
-    gets scratch of its graph's own memory, whose counters every replay clears: scratch that
-    is cached may be replaced by a larger one while the graph still refers to it."""
+def _workspace(cache: QCache, step: C.CmQattention, s, current: bool) -> torch.Tensor:
+    """Scratch of the calls enqueued on a stream (current: the current one), cached for
+    (device, stream) and allocated there, so calls on two streams never share it. A call that
+    is being captured gets scratch of its graph's own memory, whose counters every replay
+    clears: scratch that is cached may be replaced by a larger one while the graph still
+    refers to it."""
     need = ctypes.c_size_t(0)
     C.check(C.lib().cm_qcache_attention_size(ctypes.byref(cache.struct), ctypes.byref(step),
                                              ctypes.byref(need)), "cm_qcache_attention_size")
     key = (cache.device, s.cuda_stream)
     ws = _WS.get(key)
-    capturing = _capturing(s)
+    with nullcontext() if current else torch.cuda.stream(s):
+        capturing = torch.cuda.is_current_stream_capturing()
     if capturing or ws is None or ws.numel() < need.value:
         with torch.cuda.stream(s):
             ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
@@ -195,13 +197,6 @@ def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
         if not capturing:
             _WS[key] = ws
     return ws
-
-
-def _capturing(s) -> bool:
-    if s.cuda_stream == torch.cuda.current_stream(s.device).cuda_stream:
-        return torch.cuda.is_current_stream_capturing()
-    with torch.cuda.stream(s):
-        return torch.cuda.is_current_stream_capturing()
 
 
 def release_qcache_workspace() -> None:
@@ -254,7 +249,8 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
     s = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
-    ws = _workspace(cache, step, s)
+    current = stream is None and dev.index == torch.cuda.current_device()
+    ws = _workspace(cache, step, s, current)
     C.check(C.lib().cm_qcache_attention(ctypes.byref(cache.struct), layer, ctypes.byref(step),
                                         ws.data_ptr(), ws.numel(), s.cuda_stream),
             "cm_qcache_attention")
