@@ -58,7 +58,7 @@ class QCache:
 
 
 def _stream(stream, device):
-    return stream if stream is not None else torch.cuda.current_stream(device)
+    return stream if stream is not None else torch.cuda.current_stream(device.index)
 
 
 def _made_on(stream):
@@ -174,28 +174,18 @@ def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
 
 
 _WS: Dict[tuple, torch.Tensor] = {}
+_NONE = torch.empty(0, dtype=torch.uint8)
 
 
-def _workspace(cache: QCache, step: C.CmQattention, s, current: bool) -> torch.Tensor:
-    """Scratch of the calls enqueued on a stream (current: the current one), cached for
-    (device, stream) and allocated there, so calls on two streams never share it. A call that
-    is being captured gets scratch of its graph's own memory, whose counters every replay
-    clears: scratch that is cached may be replaced by a larger one while the graph still
-    refers to it."""
+def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
+    """Scratch for a call enqueued on s, allocated there."""
     need = ctypes.c_size_t(0)
     C.check(C.lib().cm_qcache_attention_size(ctypes.byref(cache.struct), ctypes.byref(step),
                                              ctypes.byref(need)), "cm_qcache_attention_size")
-    key = (cache.device, s.cuda_stream)
-    ws = _WS.get(key)
-    with nullcontext() if current else torch.cuda.stream(s):
-        capturing = torch.cuda.is_current_stream_capturing()
-    if capturing or ws is None or ws.numel() < need.value:
-        with torch.cuda.stream(s):
-            ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
-            # the calls count in it, and leave their counters at zero
-            ws[:C.CM_QCACHE_COUNTER_BYTES].zero_()
-        if not capturing:
-            _WS[key] = ws
+    with torch.cuda.stream(s):
+        ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
+        # the calls count in it, and leave their counters at zero
+        ws[:C.CM_QCACHE_COUNTER_BYTES].zero_()
     return ws
 
 
@@ -249,9 +239,20 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
     s = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
+    # Scratch is cached for (device, stream), so calls on two streams never share it, and
+    # replaced by a larger one where it is too small. A call that is being captured gets
+    # scratch of its graph's own memory, whose counters every replay clears: what is cached may
+    # be replaced while the graph still refers to it.
     current = stream is None and dev.index == torch.cuda.current_device()
-    ws = _workspace(cache, step, s, current)
-    C.check(C.lib().cm_qcache_attention(ctypes.byref(cache.struct), layer, ctypes.byref(step),
-                                        ws.data_ptr(), ws.numel(), s.cuda_stream),
-            "cm_qcache_attention")
+    with nullcontext() if current else torch.cuda.stream(s):
+        capturing = torch.cuda.is_current_stream_capturing()
+    key = (dev, s.cuda_stream)
+    ws = _workspace(cache, step, s) if capturing else _WS.get(key, _NONE)
+    args = ctypes.byref(cache.struct), layer, ctypes.byref(step)
+    f = C.lib().cm_qcache_attention
+    status = f(*args, ws.data_ptr(), ws.numel(), s.cuda_stream)
+    if status == C.CM_EWORKSPACE and not capturing:
+        ws = _WS[key] = _workspace(cache, step, s)
+        status = f(*args, ws.data_ptr(), ws.numel(), s.cuda_stream)
+    C.check(status, "cm_qcache_attention")
     return out, lse
