@@ -89,8 +89,42 @@ struct FindShared {
   Item it;
 };
 
-// The workgroup's item from the lengths: every request's context is cut into equal ranges of
-// whole units so that about `items` ranges come out for all row tiles. Every workgroup looks
+// What the rows of a tile see: positions see_lo .. see_hi - 1 of one row, those that
+// every row of the tile sees, and those that any does.
+struct Sight {
+  int tok_lo, tok_hi;      // first and last row of the request in the tile
+  int all_lo, all_hi, any_lo, any_hi;
+};
+template <int ROWS>
+__device__ __forceinline__ Sight tile_sight(const QAttention& a, const Item& it) {
+  Sight s;
+  s.tok_lo = it.tile * ROWS / a.G;
+  const int last = (it.tile * ROWS + ROWS - 1) / a.G;
+  s.tok_hi = last < it.count ? last : it.count - 1;
+  const int p_lo = it.len - it.count + s.tok_lo, p_hi = it.len - it.count + s.tok_hi;
+  s.all_hi = p_lo + 1;   // <= 0 where the first row sees nothing
+  s.all_lo = a.window && p_hi - a.window + 1 > 0 ? p_hi - a.window + 1 : 0;
+  s.any_lo = a.window && p_lo - a.window + 1 > 0 ? p_lo - a.window + 1 : 0;
+  s.any_hi = p_hi + 1 > 0 ? p_hi + 1 : 0;
+  return s;
+}
+
+// Tokens that a tile of a request sees, on the average over its tiles: a tile's last row sees the
+// rows before it, and one position more than the row before.
+template <int ROWS>
+__device__ __forceinline__ int tile_units(const QAttention& a, int count, int len) {
+  const int own = (ROWS + a.G - 1) / a.G < count ? (ROWS + a.G - 1) / a.G : count;
+  int64_t seen = (int64_t)len - (count - own) / 2;
+  if (a.window && seen > (int64_t)a.window + own) seen = (int64_t)a.window + own;
+  return seen > 0 ? (int)((seen + kUnit - 1) / kUnit) : 0;
+}
+
+// The workgroup's item from the lengths: what a request's tiles see is cut into as many equal
+// ranges of whole units that about `items` ranges come out for all row tiles, as many as run
+// together. Where there are more tiles than that, they are cut if they are longer than 3/4 of
+// what a workgroup has to do in all, beyond which the longest would be what the call waits for (six
+// prompts of 493 to 3975 rows over little, 2 heads of d = 256, G 2: 266 us uncut, 199 so); shorter
+// ones gain nothing by a cut and would cost their partial results. Every workgroup looks
 // at all n <= 1024 lengths, a few a thread: two prefix sums, about 2 us, beside which other
 // workgroups stream (a plan made once would be a launch of its own, 5 us and more). The grid and
 // the workspace hold `most` items, enough for requests that share no rows; where rows_dev lays
@@ -101,17 +135,16 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
   constexpr int kPer = CM_QCACHE_MAX_REQUESTS / THREADS;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = (a.n + THREADS - 1) / THREADS;   // requests of a thread
-  int row0[kPer], count[kPer], len[kPer], tiles[kPer], begin[kPer], units[kPer];
+  int row0[kPer], count[kPer], len[kPer], tiles[kPer], units[kPer];
   float cost = 0.f, all = 0.f;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int r = (int)threadIdx.x * per + k;
-    tiles[k] = units[k] = row0[k] = count[k] = len[k] = begin[k] = 0;
+    tiles[k] = units[k] = row0[k] = count[k] = len[k] = 0;
     if (k < per && r < a.n) {
       request(a, r, row0[k], count[k], len[k]);
       tiles[k] = row_tiles<ROWS>(a, count[k]);
-      begin[k] = visible_begin(a, count[k], len[k]);
-      units[k] = (len[k] - begin[k] + kUnit - 1) / kUnit;
+      units[k] = tile_units<ROWS>(a, count[k], len[k]);
       cost += (float)tiles[k] * (float)units[k];
       all += (float)tiles[k];
     }
@@ -133,7 +166,7 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
   // Each tile's ranges round up by about half a range, so that many fewer make `items` of them
   // in all. (And a little more than the quotient: rounded sums must not make more items than
   // the grid has.)
-  const float aim = fmaxf((float)items - 0.6f * all, 0.25f * (float)items);
+  const float aim = all <= (float)items ? (float)items - 0.6f * all : 1.333f * (float)items;
   const float want = cost / aim * 1.0001f;
   const int chunk = !a.split || want > 1e9f ? 1 << 30 : want > 1.f ? (int)want + 1 : 1;
   int splits[kPer], mine = 0;
@@ -167,8 +200,10 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
         it.row0 = row0[k];
         it.count = count[k];
         it.len = len[k];
-        it.begin = begin[k];
-        it.chunk = (int)((uint32_t)(units[k] + splits[k] - 1) / (uint32_t)splits[k]) * kUnit;
+        const Sight sight = tile_sight<ROWS>(a, it);
+        it.begin = sight.any_lo & ~63;
+        const int own = sight.any_hi > it.begin ? (sight.any_hi - it.begin + kUnit - 1) / kUnit : 0;
+        it.chunk = (int)((uint32_t)(own + splits[k] - 1) / (uint32_t)splits[k]) * kUnit;
         it.any = 1;
         lds.it = it;
       }
@@ -202,26 +237,6 @@ __device__ __forceinline__ HeadItem head_item(int H, int block) {
   return {y % H, (y / H) * 8 + x};
 }
 inline int64_t head_groups(int H, int64_t items) { return (items + 7) / 8 * 8 * H; }
-
-// What the rows of a tile see: positions see_lo .. see_hi - 1 of one row, those that
-// every row of the tile sees, and those that any does.
-struct Sight {
-  int tok_lo, tok_hi;      // first and last row of the request in the tile
-  int all_lo, all_hi, any_lo, any_hi;
-};
-template <int ROWS>
-__device__ __forceinline__ Sight tile_sight(const QAttention& a, const Item& it) {
-  Sight s;
-  s.tok_lo = it.tile * ROWS / a.G;
-  const int last = (it.tile * ROWS + ROWS - 1) / a.G;
-  s.tok_hi = last < it.count ? last : it.count - 1;
-  const int p_lo = it.len - it.count + s.tok_lo, p_hi = it.len - it.count + s.tok_hi;
-  s.all_hi = p_lo + 1;   // <= 0 where the first row sees nothing
-  s.all_lo = a.window && p_hi - a.window + 1 > 0 ? p_hi - a.window + 1 : 0;
-  s.any_lo = a.window && p_lo - a.window + 1 > 0 ? p_lo - a.window + 1 : 0;
-  s.any_hi = p_hi + 1 > 0 ? p_hi + 1 : 0;
-  return s;
-}
 
 // Eight codes (two words) as a matrix operand.
 __device__ __forceinline__ bf16x8 operand(uint32_t lo, uint32_t hi) {

@@ -34,8 +34,8 @@ QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n,
   p.few_items = per_head(groups);
   p.many_items = per_head(device_cu_count() * many_groups(d, terms));
   p.few_max = 2 * p.few_items;                       // a span's first and last segment
-  // a request's ranges round up once
-  p.many_max = many ? (int32_t)((rows + kManyRows - 1) / kManyRows + n + p.many_items) : 0;
+  // 4/3 of the items that run together, and every tile's ranges round up once
+  p.many_max = many ? (int32_t)((rows + kManyRows - 1) / kManyRows + n + p.many_items * 4 / 3 + 1) : 0;
   // (so many row tiles fill the GPU as they are; their partial results would be gigabytes)
   p.split = (int64_t)p.many_max * H <= kMostSplit;
   const size_t row = sizeof(float) * (size_t)(d + 4) * (size_t)H;
