@@ -32,6 +32,7 @@
 namespace cm {
 
 constexpr int kStep = 32;  // tokens of a wave's step
+constexpr int kSolo = 256;  // tokens up to which a wave takes a request by itself
 
 template <int D>
 struct Loaded {
@@ -77,9 +78,10 @@ __device__ __forceinline__ int few_units(const QAttention& a, int count, int len
   return units < 1 ? 1 : units;
 }
 
+// solo: the segment is this wave's alone; else all waves of the workgroup come here with it.
 template <int TERMS, int D, int WAVES>
 __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item& it, int h, int slot,
-                                                 FewShared<TERMS, D, WAVES>& lds) {
+                                                 bool solo, FewShared<TERMS, D, WAVES>& lds) {
   constexpr int DW = D / 16;                     // columns of a lane
   constexpr int ES = TERMS == 1 ? 2 : 4;         // bytes of a query element
   constexpr int PT = TERMS == 1 ? 2 : 3;         // terms of a probability
@@ -98,14 +100,14 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
   const int see_lo = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
   const Sight sight = tile_sight<kFewRows>(a, it);
 
-  // the wave's tokens: an equal part of the range, whole steps
+  // the wave's tokens: an equal part of the range (solo: all of it), whole steps
   int begin = it.begin, end = begin + it.chunk;
   const int from = sight.any_lo & ~(kStep - 1);
   begin = begin > from ? begin : from;
   end = end < sight.any_hi ? end : sight.any_hi;
   const int steps_all = end > begin ? (end - begin + kStep - 1) / kStep : 0;
-  const int share = (steps_all + WAVES - 1) / WAVES * kStep;
-  begin += wave * share;
+  const int share = (solo ? steps_all : (steps_all + WAVES - 1) / WAVES) * kStep;
+  begin += solo ? 0 : wave * share;
   end = end < begin + share ? end : begin + share;
 
   // elements of chunk c / 2, half c % 2, in the order of the K codes that a lane holds
@@ -120,7 +122,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
 #pragma unroll
       for (int w = 0; w < TERMS; ++w) lds.q[(c * TERMS + w) * 64 + lane] = q[0][w];
     }
-    __syncthreads();                             // (its readers end at the barriers below)
+    __syncthreads();                             // (its readers end at the next barrier)
   } else {
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) query(c, q[c]);
@@ -308,11 +310,13 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
     }
   }
 
-  // the waves' results as one, half of the waves to the other half at a time
+  // the waves' results as one, half of the waves to the other half at a time (where they have
+  // any: of up to WAVES steps a wave has one)
   l = lane_sum<32>(lane_sum<16>(l));
   const int en = anew(n), eg = anew(g);
 #pragma unroll
   for (int half = WAVES / 2; half >= 1; half >>= 1) {
+    if (solo || (!kShared && steps_all <= half)) continue;
     if (wave >= half && wave < 2 * half) {
       const int to = wave - half;
       float* row = &lds.acc[to][en][4 * eg * DW];
@@ -343,7 +347,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
     }
     __syncthreads();
   }
-  if (wave == 0 && live) {
+  if ((solo || wave == 0) && live) {
     const Part<D> part = part_of<D>(a, it, h, slot);
     const RowPlace place = row_place(a, it, h, it.tile * kFewRows + en);
 #pragma unroll
@@ -416,31 +420,53 @@ __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
   Item it;
   it.tile = 0;
   it.any = 1;
-  const auto look = [&](int r) {
-    request(a, r, it.row0, it.count, it.len);
-    it.r = r;
-    it.begin = visible_begin(a, it.count, it.len);
+  const int begin = u;
+  const int first_r = __builtin_amdgcn_readfirstlane(lds.first);
+  const int my_turn = __builtin_amdgcn_readfirstlane(wave);
+  // Requests of up to kSolo tokens that lie whole in the span, two of them or more: a wave takes
+  // each by itself, the next wave the next one. A segment of such a length is a chain of loads and
+  // a join of the waves that no bandwidth shortens (1000 requests of 100 tokens, 8 heads of d = 128:
+  // NEW us so, 109 by all waves one after another). Then the others, by all waves.
+  const auto short_one = [&](int from, int to) {
+    return from >= begin && to <= stop && to > from && (int64_t)(to - from) * a.few_unit <= kSolo;
   };
-  int r = __builtin_amdgcn_readfirstlane(lds.first);
-  while (u < stop) {
+  int pass = 1;
+  if constexpr (!shared_query(TERMS, D)) {
+    const int r = first_r + lane;
+    const bool is = r < a.n && short_one(lds.pos[r], lds.pos[r + 1]);
+    if (__builtin_popcountll(__ballot(is)) > 1) pass = 0;
+  }
+  const bool some_solo = pass == 0;
+  int r = first_r, turn = 0;
+  while (true) {
+    if (u >= stop) {
+      if (pass == 1) break;
+      pass = 1;
+      u = begin;
+      r = first_r;
+    }
     const int from = __builtin_amdgcn_readfirstlane(lds.pos[r]);
     const int to = __builtin_amdgcn_readfirstlane(lds.pos[r + 1]);
     if (from != to) {
-      look(r);
-      const int upto_u = to < stop ? to : stop;
-      it.begin += (u - from) * a.few_unit;
-      it.chunk = (upto_u - u) * a.few_unit;
-      u = upto_u;
-      // the spans that hold some of it
-      const int first = from / span, part = w - first;
-      it.splits = (to - 1) / span - first + 1;
-      // (in the first of them another request may come before it)
-      const auto slot = [&](int i) {
-        return i == 0 ? 2 * first + (from > first * span ? 1 : 0) : 2 * (first + i);
-      };
-      few_rows_segment<TERMS, D, WAVES>(a, it, h, slot(part), lds);
-      if (it.splits > 1)
-        finish_split<D, ES, kThreads>(a, it, h, part, it.splits, &lds.flag, slot);
+      const int u0 = u;
+      u = to < stop ? to : stop;
+      const bool solo = some_solo && short_one(from, to);
+      if (solo == (pass == 0) && (!solo || turn++ % WAVES == my_turn)) {
+        request(a, r, it.row0, it.count, it.len);
+        it.r = r;
+        it.begin = visible_begin(a, it.count, it.len) + (u0 - from) * a.few_unit;
+        it.chunk = (u - u0) * a.few_unit;
+        // the spans that hold some of it
+        const int first = from / span, part = w - first;
+        it.splits = (to - 1) / span - first + 1;
+        // (in the first of them another request may come before it)
+        const auto slot = [&](int i) {
+          return i == 0 ? 2 * first + (from > first * span ? 1 : 0) : 2 * (first + i);
+        };
+        few_rows_segment<TERMS, D, WAVES>(a, it, h, slot(part), solo, lds);
+        if (it.splits > 1)
+          finish_split<D, ES, kThreads>(a, it, h, part, it.splits, &lds.flag, slot);
+      }
     }
     ++r;
   }
