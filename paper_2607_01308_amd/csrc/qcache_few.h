@@ -32,7 +32,7 @@
 namespace cm {
 
 constexpr int kStep = 32;  // tokens of a wave's step
-constexpr int kSolo = 256;  // tokens up to which a wave takes a request by itself
+constexpr int kSolo = 512;  // tokens up to which a wave takes a request by itself
 
 template <int D>
 struct Loaded {
@@ -426,7 +426,8 @@ __device__ __forceinline__ void few_rows_span(const QAttention& a, int block,
   // Requests of up to kSolo tokens that lie whole in the span, two of them or more: a wave takes
   // each by itself, the next wave the next one. A segment of such a length is a chain of loads and
   // a join of the waves that no bandwidth shortens (1000 requests of 100 tokens, 8 heads of d = 128:
-  // NEW us so, 109 by all waves one after another). Then the others, by all waves.
+  // 61 us so, 108 by all waves one after another; 320 of 300 tokens 48, 55 where only 256 tokens
+  // count as short). Then the others, by all waves.
   const auto short_one = [&](int from, int to) {
     return from >= begin && to <= stop && to > from && (int64_t)(to - from) * a.few_unit <= kSolo;
   };
