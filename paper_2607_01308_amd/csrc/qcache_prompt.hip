@@ -1,7 +1,7 @@
 // Attention over the 8-bit paged cache for requests with many query rows: prompts and
 // questions of more rows than one 16-row tile holds.
 //
-// The same one-pass softmax as for few rows (qcache_attention.hip), with the work
+// The same one-pass softmax as for few rows (qcache_few.h), with the work
 // the other way round: a workgroup takes 128 query rows (a request's rows times the
 // group) of one KV head, each of its four waves 32 of them, and walks the context in
 // tiles of TOK tokens. A tile's codes are turned into bf16 once for all 128 rows, by 2^e of
@@ -14,7 +14,9 @@
 // or with the row's number so that the lanes of a load take all banks.
 //
 // Bound by the matrix and the vector units in about equal parts: for 32 rows and 64 tokens of
-// d = 128 a wave issues 32 products of 32 cycles and about 250 vector instructions.
+// d = 128 a wave issues 32 products of 32 cycles and about 260 vector instructions, 33 of them
+// exponentials. 4096 queries over 16384 tokens, 8 heads of d = 128, G 4: 1.34 ms, 0.92 PFLOP/s, the
+// matrix units busy 43% of the time and the vector units 55%.
 #include <type_traits>
 
 #include "qcache_few.h"
