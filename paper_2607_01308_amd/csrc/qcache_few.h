@@ -26,11 +26,12 @@
 // joined by the last workgroups to write theirs. The spans follow from the lengths in
 // device memory, which every workgroup looks at; the grid does not depend on them.
 //
-// Bound by HBM for long contexts, read in pieces of a page's head (2 KiB for 16 tokens of
-// d = 128): 64 ragged contexts, 8 heads of d = 128, G 4, 1.09 GB, 201 us, 5.4 TB/s; 264 thousand
-// tokens of one request 109 us, 5.0 TB/s. Below about 20 MB by the chain of loads from the lengths
-// to the codes and back through the join: 1280 tokens 12.5 us. (Three workgroups on a compute unit
-// in place of two: contexts of d = 64 5 to 8% faster, the long one of d = 128 6% slower.)
+// Bound by HBM for long contexts: 64 ragged contexts, 8 heads of d = 128, G 4, 1.09 GB, 201 us, 5.4
+// TB/s; 264 thousand tokens of one request 109 us, 5.0 TB/s, of each about 12 us at its start and
+// in its joins. Pages in order instead of shuffled, pages of 128 tokens, and loads two steps ahead
+// changed these by 1 to 2%; three workgroups on a compute unit made contexts of d = 64 5 to 8% faster
+// and the long one of d = 128 6% slower. Below about 20 MB bound by the chain of loads from
+// the lengths to the codes and back through the join: 1280 tokens 12.5 us.
 #pragma once
 
 #include "qcache_attention.h"
