@@ -581,8 +581,8 @@ int32_t cm_qcache_write(const cm_qcache* cache, int32_t first_layer, int32_t n_l
  * where none of its row's weights is more than 1/32 of their sum; out is rounded once.
  * q_dev, out_dev: n_rows rows of q_heads heads of d elements of dtype, 16-byte
  * aligned, strides in elements, multiples of 16 bytes. lse_dev: n_rows * q_heads fp32,
- * or NULL. max_rows: the most rows a request may have (a request's rows past it are
- * not computed). A length above table_width * B counts as that. Requests share no rows:
+ * or NULL. max_rows: the most rows a request may have (a request's rows past it, and
+ * those past n_rows, are not computed; they count among its c rows). A length above table_width * B counts as that. Requests share no rows:
  * where rows_dev lays them over one another, what the rows get is not defined, nor that they
  * get anything. g is at most 64. */
 typedef struct {

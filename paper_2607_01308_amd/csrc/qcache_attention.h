@@ -26,12 +26,14 @@ constexpr int many_groups(int d, int terms) { return d * (terms + 1) > 256 ? 1 :
 
 struct Item {
   int32_t r, tile, split, splits;  // request, row tile, range of its context, how many
-  int32_t row0, count, len;        // the request's first row, rows, tokens
+  int32_t row0, count, len;        // the request's first row, rows, tokens up to the last row
   int32_t begin, chunk;            // where its visible context begins, tokens of a range
   int32_t any;                     // 0: the grid has more workgroups than there are items
 };
 
-// A request's rows and tokens, within the bounds that the host checked.
+// A request's rows that are computed and the tokens up to the last one of them, within the bounds
+// that the host checked. The request's rows end at the last of its tokens: where rows past
+// max_rows or past the queries' end are left out, as many tokens are (and none may be left).
 __device__ __forceinline__ void request(const QAttention& a, int r, int& row0, int& count,
                                         int& len) {
   const int64_t first = a.rows ? a.rows[r] : r, next = a.rows ? a.rows[r + 1] : r + 1;
@@ -43,7 +45,7 @@ __device__ __forceinline__ void request(const QAttention& a, int r, int& row0, i
   t = t < 0 ? 0 : t > cap ? cap : t;
   row0 = (int)f;
   count = (int)c;
-  len = (int)t;
+  len = c > 0 ? (int)(t - (next - f - c)) : 0;
 }
 
 constexpr int kUnit = 128;  // tokens by which contexts are cut

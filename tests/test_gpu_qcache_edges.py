@@ -1,0 +1,46 @@
+"""The 8-bit cache's attention where its arguments reach their ends: requests with more rows than
+are computed, against 64-bit results (tests/qcache_ref.py)."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_01308_amd as cm
+from test_gpu_qcache import BF16, F32, check_attention, deal, filled, ints, queries
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,G,d,B,window,ends,most", [
+    (2, 1, 64, 16, 0, [10, 14, 29, 32], 4),              # few rows of a request are computed
+    (1, 4, 128, 32, 0, [10, 14, 29, 32], 4),
+    (2, 2, 256, 16, 20, [3, 12, 12, 17], 6),
+    (1, 2, 128, 16, 0, [70, 90, 300, 340], 40),          # many
+    (2, 4, 64, 32, 33, [70, 90, 300, 340], 40),
+    (1, 1, 256, 64, 0, [500, 640, 650, 700], 130),
+])
+def test_more_rows_than_are_computed(dtype, H, G, d, B, window, ends, most):
+    """A request's rows past max_rows and past the queries' end are not computed; the others stand at
+    the positions that the request's true number of rows gives them."""
+    starts, n_rows = [0] + ends[:-1], ends[-1] - 1       # the last request's end lies past the queries
+    counts = [b - a for a, b in zip(starts, ends)]
+    lens = [c + 3 + 50 * r for r, c in enumerate(counts)]
+    lens[1] = max(counts[1] - 2, 1)                      # its first rows stand before its first token
+    table, P = deal(lens, B, seed=d)
+    codes, scales = filled(P, H, B, d, seed=d + B)
+    q = queries(n_rows, H * G, d, dtype, seed=most)
+    out = torch.full_like(q, 7.0)
+    lse = torch.full((n_rows, H * G), 7.0, device="cuda")
+    cm.qcache_attention(cm.QCache(codes, scales), 0, q, ints(table), ints(lens), rows=ints([0] + ends),
+                        max_rows=most, window=window, out=out, lse=lse)
+    done = [min(c, most, max(n_rows - a, 0)) for a, c in zip(starts, counts)]
+    at = torch.tensor(np.concatenate([np.arange(a, a + m) for a, m in zip(starts, done)]),
+                      device="cuda")
+    # the last row computed sees as many tokens less as rows come after it
+    seen = [t - (c - m) for t, c, m in zip(lens, counts, done)]
+    check_attention(q[at], codes, scales, 0, table, seen, done, window=window,
+                    got=(out[at], lse[at]))
+    others = torch.ones(n_rows, dtype=torch.bool, device="cuda")
+    others[at] = False
+    assert bool((out[others] == 7).all()) and bool((lse[others] == 7).all())
