@@ -198,7 +198,8 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       if (e == 0) return s == 0.f ? 1.f : fabsf(s) * 0x1p127f;
       return __uint_as_float((__float_as_uint(s) & 0x7FFFFFu) | 0x3F800000u);
     };
-    my_kf = split(ks, my_ks) * a.scale_log2;
+    // (not 0, also where the softmax scale is: hidden scores are -inf times it)
+    my_kf = fmaxf(split(ks, my_ks) * a.scale_log2, 0x1p-126f);
     const float rest = split(vs, my_vs);
     my_vl = __builtin_amdgcn_logf(rest);
     my_vi = 1.f / rest;

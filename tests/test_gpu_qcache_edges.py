@@ -1,5 +1,5 @@
-"""The 8-bit cache's attention where its arguments reach their ends: requests with more rows than
-are computed, against 64-bit results (tests/qcache_ref.py)."""
+"""The 8-bit cache's attention where its arguments reach their ends (more rows than are computed, a
+scale of 0), against 64-bit results (tests/qcache_ref.py)."""
 
 import numpy as np
 import pytest
@@ -44,3 +44,17 @@ def test_more_rows_than_are_computed(dtype, H, G, d, B, window, ends, most):
     others = torch.ones(n_rows, dtype=torch.bool, device="cuda")
     others[at] = False
     assert bool((out[others] == 7).all()) and bool((lse[others] == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,G,d,B,window", [(2, 2, 128, 16, 0), (1, 4, 64, 32, 50), (1, 1, 256, 64, 0)])
+def test_scale_of_zero(dtype, H, G, d, B, window):
+    """All weights are equal: the mean of the values that a row sees, lse the logarithm of their
+    number; the same from the kernel for few rows and the one for many."""
+    lens, counts = [300, 77, 140, 90], [1, 3, 97, 40]
+    table, P = deal(lens, B, seed=1)
+    table[2, 1] = -1                                     # an evicted page
+    codes, scales = filled(P, H, B, d, seed=d)
+    q = queries(sum(counts), H * G, d, dtype, seed=d)
+    for scale in (0.0, -0.0, 1e-45):
+        check_attention(q, codes, scales, 0, table, lens, counts, window=window, scale=scale)
