@@ -103,7 +103,10 @@ __device__ __forceinline__ Sight tile_sight(const QAttention& a, const Item& it)
   s.tok_lo = it.tile * ROWS / a.G;
   const int last = (it.tile * ROWS + ROWS - 1) / a.G;
   s.tok_hi = last < it.count ? last : it.count - 1;
-  const int p_lo = it.len - it.count + s.tok_lo, p_hi = it.len - it.count + s.tok_hi;
+  // (a row before the first token counts as at -1: the differences with a window stay in range)
+  const int p0 = it.len - it.count;
+  const int p_lo = p0 + s.tok_lo > -1 ? p0 + s.tok_lo : -1;
+  const int p_hi = p0 + s.tok_hi > -1 ? p0 + s.tok_hi : -1;
   s.all_hi = p_lo + 1;   // <= 0 where the first row sees nothing
   s.all_lo = a.window && p_hi - a.window + 1 > 0 ? p_hi - a.window + 1 : 0;
   s.any_lo = a.window && p_lo - a.window + 1 > 0 ? p_lo - a.window + 1 : 0;

@@ -104,7 +104,7 @@ __device__ __forceinline__ void few_rows_segment(const QAttention& a, const Item
   const int head = h * a.G + rho % a.G;
   const int p = it.len - it.count + tok;         // its position
   const int see_hi = live && p >= 0 ? p + 1 : 0;
-  const int see_lo = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+  const int see_lo = a.window && see_hi > a.window ? see_hi - a.window : 0;
   const Sight sight = tile_sight<kFewRows>(a, it);
 
   // the wave's tokens: an equal part of the range (solo: all of it), whole steps

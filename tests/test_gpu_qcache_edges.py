@@ -1,5 +1,5 @@
 """The 8-bit cache's attention where its arguments reach their ends (more rows than are computed, a
-scale of 0), against 64-bit results (tests/qcache_ref.py)."""
+scale of 0, the widest windows), against 64-bit results (tests/qcache_ref.py)."""
 
 import numpy as np
 import pytest
@@ -58,3 +58,18 @@ def test_scale_of_zero(dtype, H, G, d, B, window):
     q = queries(sum(counts), H * G, d, dtype, seed=d)
     for scale in (0.0, -0.0, 1e-45):
         check_attention(q, codes, scales, 0, table, lens, counts, window=window, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,G,d", [(1, 1, 64), (2, 1, 128), (1, 1, 256)])
+def test_the_widest_windows(dtype, H, G, d):
+    """Windows up to the greatest that a caller can give, also for rows that stand before their
+    request's first token: the same as none."""
+    lens, counts, B = [5, 5, 0, 300], [9, 40, 3, 130], 16
+    table, P = deal(lens, B, seed=2)
+    codes, scales = filled(P, H, B, d, seed=d)
+    q = queries(sum(counts), H * G, d, dtype, seed=d)
+    none = check_attention(q, codes, scales, 0, table, lens, counts)
+    for window in (2 ** 31 - 1, 2 ** 31 - 30, 2 ** 30):
+        got = check_attention(q, codes, scales, 0, table, lens, counts, window=window)
+        assert torch.equal(got[0], none[0]) and torch.equal(got[1], none[1])
