@@ -495,7 +495,7 @@ int32_t cm_paged_workspace_size(const cm_pagedset* set, size_t* bytes_out);
  * loop does with it: cm_qcache_tables at the start of a step, cm_qcache_write and
  * cm_qcache_attention in each layer. All three take their lengths from device
  * memory, so a loop needs no host round trip and its calls can be captured into
- * a HIP graph.
+ * a HIP graph. The current device has to be the one that the cache lives on.
  *
  * codes_dev: [L][2][P][H][B][d] bytes, each an OCP e4m3 number (4 exponent bits, 3
  * mantissa bits, no infinity); page p of layer l's K is the [H][B][d] block at byte

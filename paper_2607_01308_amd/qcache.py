@@ -57,24 +57,35 @@ class QCache:
                 f"device={self.device})")
 
 
-def _stream(stream, device):
-    return stream if stream is not None else torch.cuda.current_stream(device.index)
-
-
 def _made_on(stream):
     """Where tensors that a call makes are allocated: on the stream it enqueues on."""
     return nullcontext() if stream is None else torch.cuda.stream(stream)
 
 
-def _use(stream, device, *tensors) -> ctypes.c_void_p:
-    """The stream a call enqueues on, with the tensors its kernels read and write
-    marked as in use there: their memory must not go to another tensor before that
-    work has finished, whichever stream they were allocated on."""
-    s = _stream(stream, device)
+def _use(stream, device, *tensors):
+    """The stream a call enqueues on and whether it is the current one of the current GPU,
+    with the tensors its kernels read and write marked as in use there: their memory must
+    not go to another tensor before that work has finished, whichever stream they were
+    allocated on."""
+    here = False
+    if stream is None:
+        stream = torch.cuda.current_stream(device.index)
+        here = device.index == torch.cuda.current_device()
+    elif stream.device != device:
+        raise ValueError(f"the stream is of {stream.device}, the tensors live on {device}")
     for t in tensors:
         if t is not None:
-            t.record_stream(s)
-    return s
+            t.record_stream(stream)
+    return stream, here
+
+
+def _call(s, here: bool, f, *args) -> int:
+    """f(*args) with s as the current stream, and so its GPU as the current one: the library enqueues
+    there, and a GPU's default stream has the same handle as any other's."""
+    if here:
+        return f(*args)
+    with torch.cuda.stream(s):
+        return f(*args)
 
 
 def _check(t: torch.Tensor, name: str, dtype, device, shape=None) -> torch.Tensor:
@@ -131,11 +142,11 @@ def qcache_tables(pages: int, block: int, held: torch.Tensor, new: torch.Tensor,
                           torch.empty(n + 1, dtype=i32, device=dev),
                           torch.empty(n, dtype=i32, device=dev),
                           torch.empty(4, dtype=torch.int64, device=dev))
-    s = _use(stream, dev, held, new, free, table)
-    C.check(C.lib().cm_qcache_tables(
-        pages, block, n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
-        table.data_ptr(), width, tokens, step.slots.data_ptr(), step.rows.data_ptr(),
-        step.lens.data_ptr(), step.info.data_ptr(), s.cuda_stream), "cm_qcache_tables")
+    s, here = _use(stream, dev, held, new, free, table)
+    C.check(_call(s, here, C.lib().cm_qcache_tables,
+                  pages, block, n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
+                  table.data_ptr(), width, tokens, step.slots.data_ptr(), step.rows.data_ptr(),
+                  step.lens.data_ptr(), step.info.data_ptr(), s.cuda_stream), "cm_qcache_tables")
     return step
 
 
@@ -167,25 +178,24 @@ def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
         raise TypeError(f"k and v must both be bfloat16 or float32, got {k.dtype} and {v.dtype}")
     if layers != v_layers:
         raise ValueError("k and v must have the same layers")
-    s = _use(stream, cache.device, cache.codes, cache.scales, k, v, slots)
-    C.check(C.lib().cm_qcache_write(ctypes.byref(cache.struct), layer, layers,
-                                    _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens,
-                                    slots.data_ptr(), s.cuda_stream), "cm_qcache_write")
+    s, here = _use(stream, cache.device, cache.codes, cache.scales, k, v, slots)
+    C.check(_call(s, here, C.lib().cm_qcache_write, ctypes.byref(cache.struct), layer, layers,
+                  _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens, slots.data_ptr(),
+                  s.cuda_stream), "cm_qcache_write")
 
 
 _WS: Dict[tuple, torch.Tensor] = {}
 _NONE = torch.empty(0, dtype=torch.uint8)
 
 
-def _workspace(cache: QCache, step: C.CmQattention, s) -> torch.Tensor:
-    """Scratch for a call enqueued on s, allocated there."""
+def _workspace(cache: QCache, step: C.CmQattention) -> torch.Tensor:
+    """Scratch for a call, allocated on the current stream."""
     need = ctypes.c_size_t(0)
     C.check(C.lib().cm_qcache_attention_size(ctypes.byref(cache.struct), ctypes.byref(step),
                                              ctypes.byref(need)), "cm_qcache_attention_size")
-    with torch.cuda.stream(s):
-        ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
-        # the calls count in it, and leave their counters at zero
-        ws[:C.CM_QCACHE_COUNTER_BYTES].zero_()
+    ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
+    # the calls count in it, and leave their counters at zero
+    ws[:C.CM_QCACHE_COUNTER_BYTES].zero_()
     return ws
 
 
@@ -238,21 +248,25 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         d ** -0.5 if scale is None else scale, q.data_ptr(), q.stride(0), q.stride(1),
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
-    s = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
-    # Scratch is cached for (device, stream), so calls on two streams never share it, and
-    # replaced by a larger one where it is too small. A call that is being captured gets
-    # scratch of its graph's own memory, whose counters every replay clears: what is cached may
-    # be replaced while the graph still refers to it.
-    current = stream is None and dev.index == torch.cuda.current_device()
-    with nullcontext() if current else torch.cuda.stream(s):
-        capturing = torch.cuda.is_current_stream_capturing()
-    key = (dev, s.cuda_stream)
-    ws = _workspace(cache, step, s) if capturing else _WS.get(key, _NONE)
+    s, here = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
+    C.check(_call(s, here, _attention, cache, layer, step, s), "cm_qcache_attention")
+    return out, lse
+
+
+def _attention(cache: QCache, layer: int, step: C.CmQattention, s) -> int:
+    """The call on s, which is the current stream.
+
+    Scratch is cached for (device, stream), so calls on two streams never share it, and
+    replaced by a larger one where it is too small. A call that is being captured gets
+    scratch of its graph's own memory, whose counters every replay clears: what is cached may
+    be replaced while the graph still refers to it."""
+    capturing = torch.cuda.is_current_stream_capturing()
+    key = (cache.device, s.cuda_stream)
+    ws = _workspace(cache, step) if capturing else _WS.get(key, _NONE)
     args = ctypes.byref(cache.struct), layer, ctypes.byref(step)
     f = C.lib().cm_qcache_attention
     status = f(*args, ws.data_ptr(), ws.numel(), s.cuda_stream)
     if status == C.CM_EWORKSPACE and not capturing:
-        ws = _WS[key] = _workspace(cache, step, s)
+        ws = _WS[key] = _workspace(cache, step)
         status = f(*args, ws.data_ptr(), ws.numel(), s.cuda_stream)
-    C.check(status, "cm_qcache_attention")
-    return out, lse
+    return status
