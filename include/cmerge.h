@@ -577,8 +577,7 @@ int32_t cm_qcache_write(const cm_qcache* cache, int32_t first_layer, int32_t n_l
  * A row that sees nothing gives out 0 and lse -inf. What a row does not see has no
  * effect on it, NaN included. Products, exponents and sums are in fp32. The weights
  * exp(x_j - m) enter the second product with 24 bits for fp32 queries and with 16 for
- * bf16 ones, with 8 (to nearest even) in a request of more than 16 rows of queries (rows times g)
- * where none of its row's weights is more than 1/32 of their sum; out is rounded once.
+ * bf16 ones; out is rounded once.
  * q_dev, out_dev: n_rows rows of q_heads heads of d elements of dtype, 16-byte
  * aligned, strides in elements, multiples of 16 bytes. lse_dev: n_rows * q_heads fp32,
  * or NULL. max_rows: the most rows a request may have (a request's rows past it, and

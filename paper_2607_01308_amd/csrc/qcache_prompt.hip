@@ -13,10 +13,15 @@
 // token 16 s + 8 (e / 4) + 4 k + e % 4. Chunks are moved within their rows by an exclusive
 // or with the row's number so that the lanes of a load take all banks.
 //
-// Bound by the matrix and the vector units in about equal parts: for 32 rows and 64 tokens of
-// d = 128 a wave issues 32 products of 32 cycles and about 260 vector instructions, 33 of them
-// exponentials. 4096 queries over 16384 tokens, 8 heads of d = 128, G 4: 1.34 ms, 0.92 PFLOP/s, the
-// matrix units busy 43% of the time and the vector units 55%.
+// Weights enter the second product as two bf16 terms (16 bits) for bf16 queries, three (24 bits) for
+// fp32 ones, as in the kernel for few rows. One term would cost as much error as the
+// rounding of the output does, whatever the size of the single weights, since outputs become
+// smaller as their errors do: 300 queries of nearly equal weights over 4000 tokens were
+// off by 1.49 times the output's own rounding, and 4096 queries over 16384 tokens took 1.33 ms
+// so, 1.66 ms with two.
+//
+// Bound by the matrix and the vector units: 4096 queries over 16384 tokens, 8 heads of d = 128, G 4:
+// 1.66 to 1.77 ms, 0.70 to 0.74 PFLOP/s.
 #include <type_traits>
 
 #include "qcache_few.h"
@@ -112,6 +117,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   constexpr int kWaves = kRowWaves * HALVES;
   constexpr int DH = D / HALVES;                 // columns of a wave
   constexpr int ES = TERMS == 1 ? 2 : 4;
+  constexpr int PT = TERMS == 1 ? 2 : 3;         // terms of a probability
   constexpr int kGroups = TOK / 16;              // 16-token groups of a tile
   constexpr int COLS = D * kGroups / kWaves;     // columns that a wave stages of its group
   constexpr int kTok32 = TOK / 32;
@@ -348,26 +354,22 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
       ref = top;
     }
     const float low = ref == kNone ? 0.f : ref;
-    // terms of a probability: fp32 queries take three; bf16 queries two while a single
-    // weight may be more than 1/32 of a row's sum, then one (an error of 2^-8 of 2^-5)
-    bool fine = TERMS == 3;
-    if constexpr (TERMS == 1) {
-      const float whole = lane_sum<32>(l);
-      fine = __any(live && !(whole >= 32.f * __builtin_amdgcn_exp2f(top - low)));
-    }
     const uint32_t vr = fresh(v_read);
-    // out^T += V^T P^T, 16 tokens at a time: registers 8 (s % 2) .. of sc[s / 2]
+    // out^T += V^T P^T, 16 tokens at a time: registers 8 (s % 2) .. of sc[s / 2], as the sum of
+    // PT bf16 terms, each the rounding of what the ones before have left
     const auto products = [&](int s) {
-      u32x4 w;
+      bf16x8 pt[PT];
+      float x[8];
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        w[k] = pair_bf16(sc[s >> 1][8 * (s & 1) + 2 * k], sc[s >> 1][8 * (s & 1) + 2 * k + 1]);
-      const bf16x8 pt = __builtin_bit_cast(bf16x8, w);
+      for (int i = 0; i < 8; ++i) x[i] = sc[s >> 1][8 * (s & 1) + i];
+      split_terms<PT>(x, pt);
 #pragma unroll
       for (int j = 0; j < DH / 32; ++j) {
         const int e = s * (DH / 32) + j;
-        acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[e % kAhead]), pt,
-                                                         acc[j], 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < PT; ++w)
+          acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, f[e % kAhead]),
+                                                           pt[w], acc[j], 0, 0, 0);
         if (e + kAhead < kOutOps) f[e % kAhead] = v_operand(vr, buf, e + kAhead);
       }
     };
@@ -387,22 +389,6 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
     for (int s = 0; s < kGroups; ++s) {
       if (s + 1 < kGroups) exponents(s + 1);
       products(s);
-    }
-
-    for (int more = TERMS == 3 ? 2 : fine ? 1 : 0; more > 0; --more) {
-      // what the terms so far have left of the probabilities
-#pragma unroll
-      for (int b = 0; b < kTok32; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const uint32_t w = pair_bf16(sc[b][i], sc[b][i + 1]);
-          sc[b][i] -= low_bf16(w);
-          sc[b][i + 1] -= high_bf16(w);
-        }
-#pragma unroll
-      for (int e = 0; e < kAhead; ++e) f[e] = v_operand(vr, buf, e);
-#pragma unroll
-      for (int s = 0; s < kGroups; ++s) products(s);
     }
   };
 
