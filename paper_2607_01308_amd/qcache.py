@@ -150,6 +150,16 @@ def qcache_tables(pages: int, block: int, held: torch.Tensor, new: torch.Tensor,
     return step
 
 
+def check_rows(x: torch.Tensor, name: str, device) -> None:
+    """What cm_qcache_write needs of rows [tokens, H, d] beside their shape and type."""
+    if x.device != device:
+        raise ValueError(f"{name} must live on {device}, got {x.device}")
+    if x.stride(2) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    if x.numel() and (x.data_ptr() % 16 or any(x.stride(i) * x.element_size() % 16 for i in (0, 1))):
+        raise ValueError(f"{name} must be 16-byte aligned, and its strides multiples of 16 bytes")
+
+
 def _rows(x: torch.Tensor, name: str, cache: QCache, tokens: int):
     """The layers of x and its rows as the library takes them."""
     shape, stride = x.shape, x.stride()

@@ -19,8 +19,8 @@ from typing import List, Optional, Sequence
 import torch
 
 from .binding import _DTYPES
-from .qcache import (QCache, QCacheStep, _made_on, _use, qcache_attention, qcache_tables,
-                     qcache_write)
+from .qcache import (QCache, QCacheStep, _made_on, _use, check_rows, qcache_attention,
+                     qcache_tables, qcache_write)
 
 
 @dataclass
@@ -123,7 +123,7 @@ class ServingCache:
     def load(self, place: int, layers: Sequence, stream=None) -> ServingStep:
         """Appends a merged cache to a place: per layer (K, V), each [1, H, T, d], as the
         renders return it. One write for a cache that is one buffer, else one for each
-        layer."""
+        layer. A cache that cannot be written is refused, and nothing changed."""
         if not 0 <= place < self.places:
             raise ValueError(f"place must be in [0, {self.places}), got {place}")
         H, d = self.cache.H, self.cache.d
@@ -137,13 +137,21 @@ class ServingCache:
             if K.dtype not in _DTYPES or V.dtype is not K.dtype:
                 raise TypeError(f"K and V must both be bfloat16 or float32, got {K.dtype} and "
                                 f"{V.dtype}")
+            for x, name in ((K, "K"), (V, "V")):
+                check_rows(x[0].transpose(0, 1), name, self.cache.device)
+        before = self._head, self._held, self.lengths
         step = self.extend([T if r == place else 0 for r in range(self.places)], stream)
-        k, v = (_one_buffer([pair[i] for pair in layers]) for i in (0, 1))
-        if k is not None and v is not None:
-            self.write(0, k, v, step, stream)
-        else:
-            for layer, (K, V) in enumerate(layers):
-                self.write(layer, K[0].transpose(0, 1), V[0].transpose(0, 1), step, stream)
+        try:
+            k, v = (_one_buffer([pair[i] for pair in layers]) for i in (0, 1))
+            if k is not None and v is not None:
+                self.write(0, k, v, step, stream)
+            else:
+                for layer, (K, V) in enumerate(layers):
+                    self.write(layer, K[0].transpose(0, 1), V[0].transpose(0, 1), step, stream)
+        except Exception:
+            # (the table's entries past a place's tokens and their pages are dealt again)
+            self._head, self._held, self.lengths = before
+            raise
         return step
 
 

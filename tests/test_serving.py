@@ -71,3 +71,56 @@ def test_layers_of_one_buffer():
     assert serving._one_buffer([ks[0], ks[1], ks[1]]) is None
     assert serving._one_buffer([ks[0]]) is not None
     assert serving._one_buffer([ks[0], one[1, 0, :, :, :7].double()]) is None
+
+
+class Writes:
+    """qcache_write that refuses the `bad`-th call."""
+    def __init__(self, bad):
+        self.bad, self.calls = bad, 0
+
+    def __call__(self, cache, layer, k, v, slots, stream=None):
+        self.calls += 1
+        if self.calls == self.bad:
+            raise RuntimeError("no")
+
+
+def state(sc):
+    return (list(sc.lengths), sc.free_pages, sc._held.tolist(), sc._free[sc._head:sc._tail].tolist())
+
+
+def test_caches_that_cannot_be_written_are_refused_before(plain, monkeypatch):
+    """Nothing is taken for K and V whose last dimension is strided, that are misaligned or whose
+    strides are, or that live elsewhere."""
+    sc = serving.ServingCache(FakeCache(9, 16), 2, 64)
+    writes = Writes(0)
+    monkeypatch.setattr(serving, "qcache_write", writes)
+    sc.extend([17, 3])
+    before = state(sc)
+    good = torch.zeros((1, 2, 5, 64))
+    flat = torch.zeros(1 + 2 * 5 * 64)
+    for bad in (torch.zeros((1, 2, 5, 128))[..., ::2],               # strided
+                flat[1:].view(1, 2, 5, 64),                          # a base that is not aligned
+                torch.zeros((1, 2, 5, 65))[..., :64],                # rows that are not
+                torch.zeros((1, 2, 5, 64), device="meta")):          # another device
+        for pair in ((good, bad), (bad, good)):
+            with pytest.raises(ValueError, match="K|V"):
+                sc.load(1, [(good, good), pair])
+            assert state(sc) == before and writes.calls == 0
+    sc.load(1, [(good, good)] * 2)
+    assert sc.lengths == [17, 8]
+
+
+@pytest.mark.parametrize("bad", [1, 2])
+def test_a_write_that_fails_gives_the_pages_back(plain, monkeypatch, bad):
+    sc = serving.ServingCache(FakeCache(9, 16), 2, 64)
+    sc.extend([17, 3])
+    before = state(sc)
+    monkeypatch.setattr(serving, "qcache_write", Writes(bad))
+    layers = [(torch.zeros((1, 2, 40, 64)), torch.zeros((1, 2, 40, 64))) for _ in range(2)]
+    with pytest.raises(RuntimeError, match="no"):
+        sc.load(1, layers)
+    assert state(sc) == before
+    sc.load(1, layers)                                   # the same pages again
+    assert sc.lengths == [17, 43] and plain[-1][2] == 2
+    used = [int(p) for r in range(2) for p in sc.table[r, :-(-sc.lengths[r] // 16)]]
+    assert sorted(used + sc._free[sc._head:sc._tail].tolist()) == list(range(9))
