@@ -73,7 +73,7 @@ def main(agents: int = 4, steps: int = 32, question: int = 24, block: int = 16,
         deliveries = synth.make_deliveries(w, synth.make_fragments(w, device="cuda"))
         merged.append(cm.render_deliveries(deliveries, w.routing_layer, w.rope_base).cache)
     tokens = [c[0][0].shape[2] for c in merged]
-    max_len = max(tokens) + question + steps
+    max_len = max(tokens) + question + max(steps, 4)     # (three steps untimed, one at least timed)
     pages = agents * -(-max_len // block)
     sc = cm.ServingCache(cm.QCache.empty(L, H, d, pages, block), agents, max_len)
     for a, cache in enumerate(merged):

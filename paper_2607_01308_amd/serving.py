@@ -41,7 +41,7 @@ class ServingCache:
     def __init__(self, cache: QCache, places: int, max_len: int):
         if places < 1 or max_len < 1:
             raise ValueError("places and max_len must be at least 1")
-        self.cache, self.places = cache, int(places)
+        self.cache, self.places, self.max_len = cache, int(places), int(max_len)
         self.lengths: List[int] = [0] * self.places       # tokens of each place
         dev, i32 = cache.device, torch.int32
         self.table = torch.zeros((self.places, -(-max_len // cache.B)), dtype=i32, device=dev)
@@ -66,10 +66,8 @@ class ServingCache:
         if len(new) != self.places or min(new) < 0:
             raise ValueError(f"new must be {self.places} numbers >= 0, got {list(new)}")
         after = [a + b for a, b in zip(self.lengths, new)]
-        room = self.table.shape[1]
-        if self._pages(max(after)) > room:
-            raise ValueError(f"a place would hold {max(after)} tokens, its table {room} pages of "
-                             f"{self.cache.B}")
+        if max(after) > self.max_len:
+            raise ValueError(f"a place would hold {max(after)} tokens, more than {self.max_len}")
         need = sum(self._pages(b) - self._pages(a) for a, b in zip(self.lengths, after))
         if need > self.free_pages:
             raise RuntimeError(f"the step needs {need} pages, {self.free_pages} are free")

@@ -124,3 +124,17 @@ def test_a_write_that_fails_gives_the_pages_back(plain, monkeypatch, bad):
     assert sc.lengths == [17, 43] and plain[-1][2] == 2
     used = [int(p) for r in range(2) for p in sc.table[r, :-(-sc.lengths[r] // 16)]]
     assert sorted(used + sc._free[sc._head:sc._tail].tolist()) == list(range(9))
+
+
+@pytest.mark.parametrize("max_len", [1, 15, 16, 17, 70])
+def test_places_do_not_grow_beyond_their_length(plain, max_len):
+    """To the token, also where the last page has room for more."""
+    sc = serving.ServingCache(FakeCache(20, 16), 2, max_len)
+    sc.extend([max_len, 0])
+    for new in ([1, 0], [0, max_len + 1]):
+        before = state(sc)
+        with pytest.raises(ValueError, match=f"would hold {max_len + 1} tokens"):
+            sc.extend(new)
+        assert state(sc) == before
+    sc.extend([0, max_len])
+    assert sc.lengths == [max_len, max_len]
