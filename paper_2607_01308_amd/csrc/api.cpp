@@ -1232,13 +1232,17 @@ int32_t element_bytes(int32_t dtype, int32_t* out) {
   return CM_OK;
 }
 
-// Strided rows that the kernels load in 16-byte pieces.
+// Strided rows that the kernels load in 16-byte pieces. The stride of a dimension of size 1 is
+// not used, and a caller's may be anything.
+struct Stride {
+  int64_t size, stride;
+};
 int32_t check_strides(const char* what, const void* data, int32_t esize,
-                      std::initializer_list<int64_t> strides) {
+                      std::initializer_list<Stride> strides) {
   if (!data || !aligned(data, 16))
     return fail(CM_EINVAL, std::string(what) + " is NULL or not 16-byte aligned");
-  for (int64_t s : strides)
-    if (s < 0 || s > ((int64_t)1 << 40) || (s * esize) % 16 != 0)
+  for (const Stride& s : strides)
+    if (s.stride < 0 || s.stride > ((int64_t)1 << 40) || (s.size > 1 && (s.stride * esize) % 16 != 0))
       return fail(CM_EINVAL, std::string(what) + " has a stride that is negative, above 2^40 or "
                                                  "no multiple of 16 bytes");
   return CM_OK;
@@ -1321,10 +1325,12 @@ int32_t cm_qcache_write(const cm_qcache* cache, int32_t first_layer, int32_t n_l
   if (!k || !v) return fail(CM_EINVAL, "k / v is NULL");
   if (n_tokens == 0 || n_layers == 0) return CM_OK;
   if ((st = check_strides("k", k->data_dev, esize,
-                          {k->layer_stride, k->token_stride, k->head_stride})) != CM_OK)
+                          {{n_layers, k->layer_stride}, {n_tokens, k->token_stride},
+                           {c.H, k->head_stride}})) != CM_OK)
     return st;
   if ((st = check_strides("v", v->data_dev, esize,
-                          {v->layer_stride, v->token_stride, v->head_stride})) != CM_OK)
+                          {{n_layers, v->layer_stride}, {n_tokens, v->token_stride},
+                           {c.H, v->head_stride}})) != CM_OK)
     return st;
   if (!slots_dev || !aligned(slots_dev, 8)) return fail(CM_EINVAL, "slots_dev is NULL or misaligned");
   const auto bytes = [&](const cm_qrows* r) {
@@ -1368,11 +1374,13 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
   if (!step->table_dev || !aligned(step->table_dev, 4))
     return fail(CM_EINVAL, "table_dev is NULL or misaligned");
   if (step->n_rows == 0) return CM_OK;
-  if ((st = check_strides("q_dev", step->q_dev, esize, {step->q_row_stride, step->q_head_stride})) !=
+  if ((st = check_strides("q_dev", step->q_dev, esize,
+                          {{step->n_rows, step->q_row_stride}, {step->q_heads, step->q_head_stride}})) !=
       CM_OK)
     return st;
   if ((st = check_strides("out_dev", step->out_dev, esize,
-                          {step->out_row_stride, step->out_head_stride})) != CM_OK)
+                          {{step->n_rows, step->out_row_stride},
+                           {step->q_heads, step->out_head_stride}})) != CM_OK)
     return st;
   if (step->lse_dev && !aligned(step->lse_dev, 4)) return fail(CM_EINVAL, "lse_dev is misaligned");
   const cm::QAttentionPlan plan = qattention_plan(c, step);

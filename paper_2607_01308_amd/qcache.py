@@ -156,7 +156,8 @@ def check_rows(x: torch.Tensor, name: str, device) -> None:
         raise ValueError(f"{name} must live on {device}, got {x.device}")
     if x.stride(2) != 1:
         raise ValueError(f"the last dimension of {name} must be contiguous")
-    if x.numel() and (x.data_ptr() % 16 or any(x.stride(i) * x.element_size() % 16 for i in (0, 1))):
+    if x.numel() and (x.data_ptr() % 16 or any(x.shape[i] > 1 and x.stride(i) * x.element_size() % 16
+                                               for i in (0, 1))):
         raise ValueError(f"{name} must be 16-byte aligned, and its strides multiples of 16 bytes")
 
 

@@ -73,3 +73,24 @@ def test_the_widest_windows(dtype, H, G, d):
     for window in (2 ** 31 - 1, 2 ** 31 - 30, 2 ** 30):
         got = check_attention(q, codes, scales, 0, table, lens, counts, window=window)
         assert torch.equal(got[0], none[0]) and torch.equal(got[1], none[1])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_one_token_of_unaligned_rows(dtype):
+    """Dimensions of size 1 with strides that are no multiple of 16 bytes."""
+    H, d, B = 1, 64, 16
+    k, v, q = (queries(1, 1, d, dtype, seed=i).expand(3, 1, d) for i in range(3))
+    odd = [torch.empty((3, 67), dtype=dtype, device="cuda") for _ in range(4)]
+    for to, x in zip(odd, (k, v, q)):
+        to[0, :64] = x[0, 0]
+    k, v, q, out = (x[:1, None, :64].as_strided((1, 1, d), (67, 67, 1)) for x in odd)
+    cache = cm.QCache.empty(1, H, d, 2, B)
+    table, one = ints([[1]]), ints([1])
+    cm.qcache_write(cache, 0, k, v, torch.tensor([B], device="cuda"))
+    _, lse = cm.qcache_attention(cache, 0, q, table, one, out=out)
+    same = cm.QCache.empty(1, H, d, 2, B)
+    cm.qcache_write(same, 0, k.clone().view(1, 1, d), v.clone().view(1, 1, d),
+                    torch.tensor([B], device="cuda"))
+    assert torch.equal(same.codes.view(torch.uint8), cache.codes.view(torch.uint8))
+    want = cm.qcache_attention(same, 0, q.clone().view(1, 1, d), table, one)
+    assert torch.equal(want[0], out) and torch.equal(want[1], lse)

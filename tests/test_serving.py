@@ -138,3 +138,10 @@ def test_places_do_not_grow_beyond_their_length(plain, max_len):
         assert state(sc) == before
     sc.extend([0, max_len])
     assert sc.lengths == [max_len, max_len]
+
+
+def test_one_token_of_unaligned_rows_is_loaded(plain, monkeypatch):
+    sc = serving.ServingCache(FakeCache(9, 16, L=1, H=1), 1, 64)
+    monkeypatch.setattr(serving, "qcache_write", Writes(0))
+    sc.load(0, [(torch.zeros(67).as_strided((1, 1, 1, 64), (67, 67, 67, 1)),) * 2])
+    assert sc.lengths == [1]
