@@ -36,7 +36,11 @@ class ServingStep:
 class ServingCache:
     """`places` requests at a time, of at most max_len tokens each, in the pages of
     `cache` (all of them: what they held is lost). Calls enqueue on one stream (`stream`,
-    else the current one); a caller that changes streams between calls orders them."""
+    else the current one); a caller that changes streams between calls orders them.
+
+    The lengths and the free pages move on with each extend, load and release on the host, so
+    these are not captured into a HIP graph, whose replays would deal out the same pages
+    again; write and attend of a step may be."""
 
     def __init__(self, cache: QCache, places: int, max_len: int):
         if places < 1 or max_len < 1:
@@ -56,12 +60,20 @@ class ServingCache:
     def free_pages(self) -> int:
         return self._tail - self._head
 
+    def _refuse_capture(self, what: str, stream) -> None:
+        if self._held.is_cuda:
+            with _made_on(stream):
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError(f"{what} cannot be captured into a graph: its replays would "
+                                       "not move on")
+
     def _pages(self, tokens: int) -> int:
         return -(-tokens // self.cache.B)
 
     def extend(self, new: Sequence[int], stream=None) -> ServingStep:
         """Room for new[r] more tokens in each place r. The step is refused, and nothing
         changed, if a place would grow beyond max_len or the free pages do not suffice."""
+        self._refuse_capture("extend", stream)
         new = tuple(int(x) for x in new)
         if len(new) != self.places or min(new) < 0:
             raise ValueError(f"new must be {self.places} numbers >= 0, got {list(new)}")
@@ -86,6 +98,7 @@ class ServingCache:
         """Empties a place; its pages are free again, after the work enqueued so far."""
         if not 0 <= place < self.places:
             raise ValueError(f"place must be in [0, {self.places}), got {place}")
+        self._refuse_capture("release", stream)
         pages = self._pages(self.lengths[place])
         if pages == 0:
             return
