@@ -530,7 +530,7 @@ typedef struct {
  * every slot is -1, rows_dev is 0 and lens_dev is held (0 where that is negative), so
  * that the calls below do nothing for the step. The call itself returns CM_OK.
  * 1 <= n <= CM_QCACHE_MAX_REQUESTS; slots_dev and info_dev are 8-byte aligned, the
- * others 4-byte. */
+ * others 4-byte. What is written overlaps nothing that is read: lens_dev is not held_dev. */
 int32_t cm_qcache_tables(int64_t pages, int32_t block, int32_t n, const int32_t* held_dev,
                          const int32_t* new_dev, const int32_t* free_dev, int64_t n_free,
                          int32_t* table_dev, int64_t table_width, int64_t n_tokens,

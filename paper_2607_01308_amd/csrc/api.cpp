@@ -1303,6 +1303,23 @@ int32_t cm_qcache_tables(int64_t pages, int32_t block, int32_t n, const int32_t*
   if (!rows_dev || !lens_dev || !aligned(rows_dev, 4) || !aligned(lens_dev, 4))
     return fail(CM_EINVAL, "rows_dev / lens_dev NULL or misaligned");
   if (!info_dev || !aligned(info_dev, 8)) return fail(CM_EINVAL, "info_dev is NULL or misaligned");
+  // every workgroup reads the lengths and the free list, some after others have written
+  struct Range {
+    const void* at;
+    int64_t bytes;
+    const char* name;
+  };
+  const Range read[] = {{held_dev, 4ll * n, "held_dev"}, {new_dev, 4ll * n, "new_dev"},
+                        {free_dev, 4 * n_free, "free_dev"}};
+  const Range written[] = {{table_dev, 4 * n * table_width, "table_dev"}, {slots_dev, 8 * n_tokens, "slots_dev"},
+                           {rows_dev, 4ll * (n + 1), "rows_dev"}, {lens_dev, 4ll * n, "lens_dev"},
+                           {info_dev, 32, "info_dev"}};
+  for (const Range& w : written)
+    for (const Range& r : read) {
+      const uintptr_t a = reinterpret_cast<uintptr_t>(w.at), b = reinterpret_cast<uintptr_t>(r.at);
+      if (a < b + (uintptr_t)r.bytes && b < a + (uintptr_t)w.bytes)
+        return fail(CM_EINVAL, std::string(w.name) + " overlaps " + r.name);
+    }
   hipError_t e = cm::launch_qcache_tables(pages, __builtin_ctz((unsigned)block), n, held_dev,
                                           new_dev, free_dev, n_free, table_dev, table_width,
                                           n_tokens, slots_dev, rows_dev, lens_dev, info_dev,
