@@ -1437,12 +1437,12 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
   a.few_max = plan.few_max;
   a.many_items = plan.many_items;
   a.many_max = plan.many_max;
+  a.many_places = plan.many_places;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.few_part = reinterpret_cast<float*>(ws + plan.few_at);
   a.many_part = reinterpret_cast<float*>(ws + plan.many_at);
   a.many_found = ws + plan.found_at;
   a.few_count = reinterpret_cast<int32_t*>(ws);
-  a.split = plan.split;
   hipError_t e = cm::launch_qcache_attention(a, c.d, step->dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_attention");
 }

@@ -44,14 +44,14 @@ struct QAttention {
   int32_t negate;     // the softmax scale is negative
   // For requests of few query rows and of many: the spans (few) or items (many) that their
   // contexts are cut into for each KV head, places of partial results for each KV head,
-  // where they are, [H][max], and the counters of those for few, [H][max][2].
-  int32_t few_items, few_max, many_items, many_max;
+  // where they are, [H][few_max] and [H][many_places], and the counters of those for few,
+  // [H][few_max][2]; the most items of many rows for each KV head.
+  int32_t few_items, few_max, many_items, many_max, many_places;
   float* few_part;
   float* many_part;
-  void* many_found;   // the items of many rows, [many_max]
+  void* many_found;   // the items of many rows that have a place, [many_places]
   int32_t* few_count;
   int32_t few_unit;   // tokens by which few rows' contexts are cut
-  int32_t split;      // 0: no request of many rows is cut
 };
 
 hipError_t launch_qcache_tables(int64_t pages, int32_t b_shift, int32_t n, const int32_t* held,
@@ -66,10 +66,9 @@ hipError_t launch_qcache_write(const QCacheDesc& c, int32_t first_layer, int32_t
 // sizes its grid and its workspace, from what the host knows.
 // counters at the start of the workspace; 4 H or 2048 are used
 constexpr int64_t kCounters = CM_QCACHE_COUNTER_BYTES / (int64_t)sizeof(int32_t);
-constexpr int64_t kMostSplit = 1 << 16;  // items of many rows, beyond which none is cut
 struct QAttentionPlan {
   int32_t few_unit, few_items, few_max, many_items, many_max;
-  bool split;
+  int32_t many_places;  // 0: no request of many rows is cut
   size_t few_at, found_at, many_at, bytes;  // partial results in the workspace, its size
 };
 QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows,

@@ -29,6 +29,7 @@ struct Item {
   int32_t row0, count, len;        // the request's first row, rows, tokens up to the last row
   int32_t begin, chunk;            // where its visible context begins, tokens of a range
   int32_t any;                     // 0: the grid has more workgroups than there are items
+  int32_t place, places;           // of its partial results where splits > 1; how many there are in all
 };
 
 // A request's rows that are computed and the tokens up to the last one of them, within the bounds
@@ -87,7 +88,7 @@ __device__ __forceinline__ int row_tiles(const QAttention& a, int count) {
 // What the workgroup shares while it looks for its item.
 struct FindShared {
   float cost[8], tiles[8];
-  int items[8];
+  int items[8], places[8];
   Item it;
 };
 
@@ -131,9 +132,10 @@ __device__ __forceinline__ int tile_units(const QAttention& a, int count, int le
 // prompts of 493 to 3975 rows over little, 2 heads of d = 256, G 2: 266 us uncut, 199 so); shorter
 // ones gain nothing by a cut and would cost their partial results. Every workgroup looks
 // at all n <= 1024 lengths, a few a thread: two prefix sums, about 2 us, beside which other
-// workgroups stream (a plan made once would be a launch of its own, 5 us and more). The grid and
-// the workspace hold `most` items, enough for requests that share no rows; where rows_dev lays
-// requests over one another so that more come out, no workgroup has an item.
+// workgroups stream (a plan made once would be a launch of its own, 5 us and more). The grid holds
+// `most` items, enough for requests that share no rows, and the workspace a.many_places of the items
+// that cut tiles have, one after another; where rows_dev lays requests over one another so that
+// more come out, no workgroup has an item.
 template <int ROWS, int THREADS>
 __device__ __forceinline__ Item find_item(const QAttention& a, int items, int most, int item,
                                           FindShared& lds) {
@@ -156,7 +158,7 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
   }
   cost = wave_scan(cost);
   all = wave_scan(all);
-  if (threadIdx.x == 0) lds.it.any = 0;
+  if (threadIdx.x == 0) lds.it.any = lds.it.places = 0;
   if (lane == 63) {
     lds.cost[wave] = cost;
     lds.tiles[wave] = all;
@@ -173,25 +175,35 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
   // the grid has.)
   const float aim = all <= (float)items ? (float)items - 0.6f * all : 1.333f * (float)items;
   const float want = cost / aim * 1.0001f;
-  const int chunk = !a.split || want > 1e9f ? 1 << 30 : want > 1.f ? (int)want + 1 : 1;
-  int splits[kPer], mine = 0;
+  const int chunk = !a.many_places || want > 1e9f ? 1 << 30 : want > 1.f ? (int)want + 1 : 1;
+  int splits[kPer], mine = 0, kept = 0;          // items; those that have a place
   if (all > (float)most) return Item{};          // (their number might not fit an int)
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     splits[k] = (int)((uint32_t)(units[k] + chunk - 1) / (uint32_t)chunk);
     splits[k] = splits[k] < 1 ? 1 : splits[k];
     mine += tiles[k] * splits[k];
+    kept += splits[k] > 1 ? tiles[k] * splits[k] : 0;
   }
-  const int upto = wave_scan(mine);
-  if (lane == 63) lds.items[wave] = upto;
+  const int upto = wave_scan(mine), kept_upto = wave_scan(kept);
+  if (lane == 63) {
+    lds.items[wave] = upto;
+    lds.places[wave] = kept_upto;
+  }
   __syncthreads();
-  int at = upto - mine, total = 0;
+  int at = upto - mine, total = 0, place = kept_upto - kept, places = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 64; ++w) {
-    if (w < wave) at += lds.items[w];
+    if (w < wave) {
+      at += lds.items[w];
+      place += lds.places[w];
+    }
     total += lds.items[w];
+    places += lds.places[w];
   }
-  if (total <= most && item >= at && item < at + mine) {
+  const bool fits = total <= most && places <= a.many_places;
+  if (fits && threadIdx.x == 0) lds.it.places = places;
+  if (fits && item >= at && item < at + mine) {
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
       const int here = tiles[k] * splits[k];
@@ -210,9 +222,12 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
         const int own = sight.any_hi > it.begin ? (sight.any_hi - it.begin + kUnit - 1) / kUnit : 0;
         it.chunk = (int)((uint32_t)(own + splits[k] - 1) / (uint32_t)splits[k]) * kUnit;
         it.any = 1;
+        it.place = place + (item - at);
+        it.places = places;
         lds.it = it;
       }
       at += here;
+      place += splits[k] > 1 ? here : 0;
     }
   }
   __syncthreads();
@@ -228,6 +243,8 @@ __device__ __forceinline__ Item find_item(const QAttention& a, int items, int mo
   it.begin = same(it.begin);
   it.chunk = same(it.chunk);
   it.any = same(it.any);
+  it.place = same(it.place);
+  it.places = same(it.places);
   return it;
 }
 

@@ -36,13 +36,17 @@ QAttentionPlan plan_qcache_attention(int32_t H, int32_t d, int32_t G, int32_t n,
   p.few_max = 2 * p.few_items;                       // a span's first and last segment
   // 4/3 of the items that run together, and every tile's ranges round up once
   p.many_max = many ? (int32_t)((rows + kManyRows - 1) / kManyRows + n + p.many_items * 4 / 3 + 1) : 0;
-  // (so many row tiles fill the GPU as they are; their partial results would be gigabytes)
-  p.split = (int64_t)p.many_max * H <= kMostSplit;
+  // Partial results of the items of cut tiles alone. Such a tile sees more units than a range has, so
+  // its ranges are less than twice the quotient, and the quotients' sum is at most 4/3
+  // many_items (find_item). Where there are more heads than items that run together, no tile is
+  // cut.
+  const int32_t most = p.many_items > 1 ? p.many_items * 8 / 3 + 1 : 0;
+  p.many_places = p.many_max < most ? p.many_max : most;
   const size_t row = sizeof(float) * (size_t)(d + 4) * (size_t)H;
   p.few_at = sizeof(int32_t) * kCounters;
   p.found_at = p.few_at + align_up(row * kFewRows * (size_t)p.few_max, kWsAlign);
-  p.many_at = p.found_at + align_up(p.split ? sizeof(Item) * (size_t)p.many_max : 0, kWsAlign);
-  p.bytes = p.many_at + (p.split ? row * kManyRows * (size_t)p.many_max : 0);
+  p.many_at = p.found_at + align_up(sizeof(Item) * (size_t)p.many_places, kWsAlign);
+  p.bytes = p.many_at + row * kManyRows * (size_t)p.many_places;
   return p;
 }
 

@@ -104,7 +104,7 @@ template <int D>
 __device__ __forceinline__ ManyPart<D> many_part(const QAttention& a, const Item& it, int h,
                                                  int place) {
   const int rows = it.count * a.G - it.tile * kManyRows;
-  return {a.many_part + ((int64_t)h * a.many_max + place) * ManyPart<D>::kFloats,
+  return {a.many_part + ((int64_t)h * a.many_places + place) * ManyPart<D>::kFloats,
           rows < kManyRows ? rows : kManyRows};
 }
 
@@ -129,8 +129,12 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const HeadItem hi = head_item(a.H, block);
   const int h = hi.h, item = hi.item;
   const Item it = find_item<kManyRows, 64 * kWaves>(a, a.many_items, a.many_max, item, lds.find);
-  if (a.split && h == 0 && item < a.many_max && threadIdx.x == 0)
-    reinterpret_cast<Item*>(a.many_found)[item] = it;
+  // (where its partial results go, for the join; a place that nobody has is marked so)
+  if (h == 0 && threadIdx.x == 0) {
+    Item* found = reinterpret_cast<Item*>(a.many_found);
+    if (it.any && it.splits > 1) found[it.place] = it;
+    if (item >= it.places && item < a.many_places) found[item].any = 0;
+  }
   if (!it.any) return;
 
   // the lane's query row
@@ -521,7 +525,7 @@ __device__ __forceinline__ void many_rows_item(const QAttention& a, int block,
   const int end_row = ew % kRowWaves * kWaveRows + en;
   if (live) {
     const RowPlace place = row_place(a, it, h, it.tile * kManyRows + end_row);
-    const ManyPart<D> part = many_part<D>(a, it, h, item);
+    const ManyPart<D> part = many_part<D>(a, it, h, it.place);
 #pragma unroll
     for (int j = 0; j < DH / 32; ++j)
 #pragma unroll
@@ -562,9 +566,9 @@ constexpr int kJoinGroups = 4, kJoinThreads = 256;
 template <int D, int ES>
 __global__ __launch_bounds__(kJoinThreads) void qcache_join_kernel(QAttention a) {
   const HeadItem hi = head_item(a.H, blockIdx.x);
-  if (hi.item >= a.many_max) return;
+  if (hi.item >= a.many_places) return;
   const Item it = reinterpret_cast<const Item*>(a.many_found)[hi.item];
-  if (!it.any || it.splits == 1) return;
+  if (!it.any) return;
   const ManyPart<D> p0 = many_part<D>(a, it, hi.h, hi.item - it.split);
   const int total = p0.rows * (D / 4);
   const int parts = it.splits * kJoinGroups, part = it.split * kJoinGroups + (int)blockIdx.y;
@@ -609,9 +613,10 @@ hipError_t launch_qcache_any_rows(const QAttention& a, uint32_t many, uint32_t f
   hipLaunchKernelGGL((qcache_any_rows_kernel<TERMS, D, TOK, HALVES>), dim3(many + few),
                      dim3(64 * kRowWaves * HALVES), 0, stream, a, many);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.split) return e;
-  hipLaunchKernelGGL((qcache_join_kernel<D, TERMS == 1 ? 2 : 4>), dim3(many, kJoinGroups),
-                     dim3(kJoinThreads), 0, stream, a);
+  if (e != hipSuccess || !a.many_places) return e;
+  hipLaunchKernelGGL((qcache_join_kernel<D, TERMS == 1 ? 2 : 4>),
+                     dim3((uint32_t)head_groups(a.H, a.many_places), kJoinGroups), dim3(kJoinThreads), 0,
+                     stream, a);
   return hipGetLastError();
 }
 

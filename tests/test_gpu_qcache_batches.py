@@ -58,3 +58,21 @@ def test_more_row_tiles_than_are_cut():
         i = torch.tensor(at, device="cuda")
         check_attention(q[i], codes, scales, 0, table[some], [lens[r] for r in some],
                         [each] * len(some), got=(out[i], lse[i]), device="cuda")
+
+
+def test_a_long_request_among_more_row_tiles_than_run_together():
+    """It is cut, however many tiles there are beside it."""
+    H, G, d, B, n, each = 64, 1, 64, 16, 1010, 20
+    lens = [20 + r % 17 for r in range(n)]
+    lens[400] = 30001
+    table, P = deal(lens, B, seed=4)
+    codes, scales = filled(P, H, B, d, seed=4)
+    q = queries(n * each, H * G, d, BF16, seed=4)
+    rows = ints(np.arange(n + 1) * each)
+    out, lse = cm.qcache_attention(cm.QCache(codes, scales), 0, q, ints(table), ints(lens), rows=rows,
+                                   max_rows=each)
+    for some in ([0, 1, 2], [399, 400, 401], [n - 1]):
+        at = np.concatenate([np.arange(r * each, (r + 1) * each) for r in some])
+        i = torch.tensor(at, device="cuda")
+        check_attention(q[i], codes, scales, 0, table[some], [lens[r] for r in some],
+                        [each] * len(some), got=(out[i], lse[i]), device="cuda")

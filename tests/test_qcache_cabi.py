@@ -205,3 +205,21 @@ def test_refusals_under_sanitizers():
     assert r.returncode == 0, out
     assert "AddressSanitizer" not in r.stderr and "runtime error" not in r.stderr, out
     assert " passed" in r.stdout, out
+
+
+@pytest.mark.parametrize("H,d,G,dtype", [(8, 128, 4, C.CM_BF16), (8, 256, 4, C.CM_BF16), (1, 128, 8, C.CM_F32),
+                                         (64, 64, 1, C.CM_BF16), (300, 128, 1, C.CM_F32)])
+def test_workspace_does_not_grow_with_the_rows(lib, H, d, G, dtype):
+    """Partial results are of cut tiles alone, whose items are as many as the GPU runs together, not as
+    many as there are rows."""
+    def need(n, rows):
+        return size(lib, cache(H=H, d=d, L=1), step(n=n, q_heads=H * G, dtype=dtype, n_rows=rows,
+                                                    rows_dev=0x111000, max_rows=rows))
+
+    sizes = []
+    for n, rows in ((1, 1), (3, 60), (1, 4096), (1, 16384), (1, 250000), (1024, 200), (1024, 200000)):
+        st, bytes = need(n, rows)
+        assert st == C.CM_OK
+        sizes.append(bytes)
+    assert sizes[3] == sizes[4] == sizes[6] and max(sizes) == sizes[3]
+    assert max(sizes) < 160 << 20
