@@ -1,5 +1,6 @@
 """The 8-bit cache's attention where its arguments reach their ends (more rows than are computed, a
-scale of 0, the widest windows), against 64-bit results (tests/qcache_ref.py)."""
+scale of 0, the widest windows and groups, strides that are not used), against 64-bit results
+(tests/qcache_ref.py)."""
 
 import numpy as np
 import pytest
@@ -94,3 +95,17 @@ def test_one_token_of_unaligned_rows(dtype):
     assert torch.equal(same.codes.view(torch.uint8), cache.codes.view(torch.uint8))
     want = cm.qcache_attention(same, 0, q.clone().view(1, 1, d), table, one)
     assert torch.equal(want[0], out) and torch.equal(want[1], lse)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,G,d,B,counts", [
+    (2, 17, 64, 16, [1, 1, 1, 1]), (1, 32, 128, 16, [1, 0, 1, 1]), (1, 64, 128, 32, [1, 1, 2, 1]),
+    (2, 64, 256, 16, [1, 1, 0, 1]), (1, 48, 64, 64, [3, 1, 17, 0])])
+def test_wide_groups(dtype, H, G, d, B, counts):
+    """17 to 64 query heads for a KV head: a decoding step's row is more than a tile of 16."""
+    lens = [700, 1, 33, 5000]
+    table, P = deal(lens, B, seed=G)
+    codes, scales = filled(P, H, B, d, seed=G)
+    q = queries(sum(counts), H * G, d, dtype, seed=G)
+    for window in (0, 100):
+        check_attention(q, codes, scales, 0, table, lens, counts, window=window, device="cuda")
