@@ -91,3 +91,14 @@ def test_streams_of_another_gpu_are_refused(calls):
     with pytest.raises(ValueError, match="stream is of cuda:0"):
         three_calls(Stream(HERE, 5))
     assert calls == []
+
+
+def test_capturing_is_looked_for_on_the_caches_gpu(calls, monkeypatch):
+    from paper_2607_01308_amd import serving
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing",
+                        lambda: torch.cuda.current_device() == 1)
+    sc = object.__new__(serving.ServingCache)
+    sc._held = on_gpu(2, dtype=torch.int32)
+    for stream in (None, Stream(THERE, 5)):
+        with pytest.raises(RuntimeError, match="captured"):
+            sc._refuse_capture("extend", stream)
