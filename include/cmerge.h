@@ -605,7 +605,7 @@ typedef struct {
   int64_t table_width;
 } cm_qattention;
 
-/* Workspace: cm_qcache_attention_size() bytes (n, n_rows, max_rows, table_width,
+/* Workspace: cm_qcache_attention_size() bytes (n, n_rows, max_rows, table_width, dtype,
  * q_heads and the cache's shape decide it, not the lengths), 256-byte aligned. Its first
  * CM_QCACHE_COUNTER_BYTES must be zero before its first use, and it is used for nothing
  * else: a call counts there which parts of the step are done, and leaves the counters at

@@ -16,12 +16,13 @@ __host__ __device__ __forceinline__ bool few_rows(int64_t rows) { return rows <=
 
 // Waves that share their rows in the kernel for many (qcache_prompt.hip). A wave's registers hold
 // its queries' terms, d * terms / 4 of them, and its columns of the output, d / 2. For d = 256 two
-// waves share (one wave for all columns and half as many waves: 4096 queries over 16384 tokens 3%
-// slower, short questions 10%).
+// waves share (one wave for all columns and half as many waves: 4096 queries over 16384 tokens, 8
+// heads, G 4, 4.31 ms, so 4.11; short questions 72 us, so 67).
 constexpr int many_halves(int d) { return d > 128 ? 2 : 1; }
 
 // Workgroups of that kernel on a compute unit. Three terms of d = 128 take the registers of two
-// waves (two waves that share rows instead: 1024 queries over 16384 tokens 948 us, so 797).
+// waves (two waves that share rows instead: 1024 queries over 16384 tokens, 8 heads, G 4, 893 us,
+// so 737).
 constexpr int many_groups(int d, int terms) { return d * (terms + 1) > 256 ? 1 : 2; }
 
 struct Item {
@@ -129,7 +130,7 @@ __device__ __forceinline__ int tile_units(const QAttention& a, int count, int le
 // ranges of whole units that about `items` ranges come out for all row tiles, as many as run
 // together. Where there are more tiles than that, they are cut if they are longer than 3/4 of
 // what a workgroup has to do in all, beyond which the longest would be what the call waits for (six
-// prompts of 493 to 3975 rows over little, 2 heads of d = 256, G 2: 266 us uncut, 199 so); shorter
+// prompts of 493 to 3975 rows over up to 300 tokens, 2 heads of d = 256, G 2: 307 us uncut, 242 so); shorter
 // ones gain nothing by a cut and would cost their partial results. Every workgroup looks
 // at all n <= 1024 lengths, a few a thread: two prefix sums, about 2 us, beside which other
 // workgroups stream (a plan made once would be a launch of its own, 5 us and more). The grid holds

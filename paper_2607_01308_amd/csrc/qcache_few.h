@@ -31,7 +31,8 @@
 // in its joins. Pages in order instead of shuffled, pages of 128 tokens, and loads two steps ahead
 // changed these by 1 to 2%; three workgroups on a compute unit made contexts of d = 64 5 to 8% faster
 // and the long one of d = 128 6% slower. Below about 20 MB bound by the chain of loads from
-// the lengths to the codes and back through the join: 1280 tokens 12.5 us.
+// the lengths (twice: for the spans, and for the request) to the codes and back through the join:
+// 1280 tokens 12.5 us.
 #pragma once
 
 #include "qcache_attention.h"

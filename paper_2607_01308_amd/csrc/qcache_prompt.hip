@@ -20,8 +20,10 @@
 // off by 1.49 times the output's own rounding, and 4096 queries over 16384 tokens took 1.33 ms
 // so, 1.66 ms with two.
 //
-// Bound by the matrix and the vector units: 4096 queries over 16384 tokens, 8 heads of d = 128, G 4:
-// 1.66 to 1.77 ms, 0.70 to 0.74 PFLOP/s.
+// Bound by the vector and the matrix units: for 32 rows and 64 tokens of d = 128 a wave issues 48
+// products of 32 cycles and about 325 vector instructions, 33 of them exponentials. 4096
+// queries over 16384 tokens, 8 heads of d = 128, G 4: 1.66 to 1.77 ms, 0.70 to 0.74 PFLOP/s, the vector
+// units busy 59% of the time and the matrix units 55%.
 #include <type_traits>
 
 #include "qcache_few.h"

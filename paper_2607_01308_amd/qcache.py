@@ -223,9 +223,10 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
     returns (out, lse). table [n, width], lens [n]: each request's pages and tokens, the
     step's own included; rows [n + 1]: where each request's query rows begin (None: one
     row for each request); max_rows: the most rows of a request (default: all of them,
-    or 1 without rows); scale: of the scores (default d ** -0.5); window: positions
-    that a query sees, itself included (0: all up to its own). out: q's shape and type;
-    lse [rows, q_heads] float32 (made if not given)."""
+    or 1 without rows; the host does not see rows, so a decoding step that gives rows and
+    not max_rows goes the slower way of prompts); scale: of the scores (default
+    d ** -0.5); window: positions that a query sees, itself included (0: all up to its
+    own). out: q's shape and type; lse [rows, q_heads] float32 (made if not given)."""
     dev = cache.device
     if q.dim() != 3 or q.shape[2] != cache.d:
         raise ValueError(f"q must be [rows, q_heads, {cache.d}], got {list(q.shape)}")

@@ -133,7 +133,11 @@ class ServingCache:
     def load(self, place: int, layers: Sequence, stream=None) -> ServingStep:
         """Appends a merged cache to a place: per layer (K, V), each [1, H, T, d], as the
         renders return it. One write for a cache that is one buffer, else one for each
-        layer. A cache that cannot be written is refused, and nothing changed."""
+        layer. A cache that cannot be written is refused, and nothing changed.
+
+        The tokens come after those that the place holds, but K is written as it is: a merged
+        cache's keys are rotated for positions from 0, so queries rotated for the place's
+        positions see it right in an empty place alone."""
         if not 0 <= place < self.places:
             raise ValueError(f"place must be in [0, {self.places}), got {place}")
         H, d = self.cache.H, self.cache.d
