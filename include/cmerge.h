@@ -540,8 +540,8 @@ int32_t cm_qcache_tables(int64_t pages, int32_t block, int32_t n, const int32_t*
 /* K or V rows of a step: row t of head h of the l-th layer written starts at element
  * l * layer_stride + t * token_stride + h * head_stride of data and holds d
  * consecutive elements. data is 16-byte aligned and the strides are multiples of 16
- * bytes, but for that of a dimension of size 1, which is not used. (A merged cache [L][2][1][H][T][d] is layer_stride 2HTd, token_stride d,
- * head_stride Td.) */
+ * bytes, but for that of a dimension of size 1, which is not used. (A merged cache
+ * [L][2][1][H][T][d] is layer_stride 2HTd, token_stride d, head_stride Td.) */
 typedef struct {
   const void* data_dev;
   int64_t layer_stride;
@@ -579,10 +579,11 @@ int32_t cm_qcache_write(const cm_qcache* cache, int32_t first_layer, int32_t n_l
  * exp(x_j - m) enter the second product with 24 bits for fp32 queries and with 16 for
  * bf16 ones; out is rounded once.
  * q_dev, out_dev: n_rows rows of q_heads heads of d elements of dtype, 16-byte
- * aligned, strides in elements, multiples of 16 bytes where there is more than one. lse_dev: n_rows * q_heads fp32,
- * or NULL. max_rows: the most rows a request may have (a request's rows past it, and
- * those past n_rows, are not computed; they count among its c rows). A length above table_width * B counts as that. Requests share no rows:
- * where rows_dev lays them over one another, what the rows get is not defined, nor that they
+ * aligned, strides in elements, multiples of 16 bytes where there is more than one.
+ * lse_dev: n_rows * q_heads fp32, or NULL. max_rows: the most rows a request may have (a
+ * request's rows past it, and those past n_rows, are not computed; they count among its
+ * c rows). A length above table_width * B counts as that. Requests share no rows: where
+ * rows_dev lays them over one another, what the rows get is not defined, nor that they
  * get anything. g is at most 64. */
 typedef struct {
   int32_t n;           /* requests */

@@ -7,7 +7,8 @@ for values of either sign adds up to at most about eps * S, S = (sum_j w_j^2 v_j
 mean square over a head's columns. eps is made of
   2^-21                 exp2, the sums of the waves and the final quotient, two units each
   2^-23 Y               the score: products are exact, their sum, the scale's factor and the
-                        maximum's subtraction are rounded in fp32; Y = max_j |x_j| + |scale| (sum_i q_i^2 k_ij^2)^(1/2)
+                        maximum's subtraction are rounded in fp32;
+                        Y = max_j |x_j| + |scale| (sum_i q_i^2 k_ij^2)^(1/2)
   2^-24 (3 T / 16)^(1/2) the sums over T tokens, 16 and one of three terms at a time, at most 2048 in
                         a row (longer contexts are cut)
   2^-18                 for bf16 queries, whose weights are two bf16 terms (2^-9 of 2^-9)
@@ -47,6 +48,9 @@ def attend(q, codes, scales, table, lens, counts, window=0, scale=None, weights=
     S, Y = torch.zeros_like(lse), torch.zeros_like(lse)
     at = 0
     for r, (T, count) in enumerate(zip(lens, counts)):
+        if T < 1 or count < 1:
+            at += count
+            continue
         pages = torch.as_tensor(table[r][:-(-T // B)], dtype=torch.long, device=dev)
         k, v = ((lut[codes[w, pages].long()] * scales[w, pages].double()[:, :, None, None])
                 .transpose(0, 1).reshape(H, -1, d)[:, :T] for w in (0, 1))
