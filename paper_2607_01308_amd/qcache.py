@@ -63,28 +63,25 @@ def _made_on(stream):
 
 
 def _use(stream, device, *tensors):
-    """The stream a call enqueues on and whether it is the current one of the current GPU,
-    with the tensors its kernels read and write marked as in use there: their memory must
-    not go to another tensor before that work has finished, whichever stream they were
-    allocated on."""
-    here = False
+    """The stream a call enqueues on and whether its GPU is the current one, with the tensors
+    its kernels read and write marked as in use there: their memory must not go to another
+    tensor before that work has finished, whichever stream they were allocated on."""
     if stream is None:
         stream = torch.cuda.current_stream(device.index)
-        here = device.index == torch.cuda.current_device()
     elif stream.device != device:
         raise ValueError(f"the stream is of {stream.device}, the tensors live on {device}")
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
-    return stream, here
+    return stream, device.index == torch.cuda.current_device()
 
 
-def _call(s, here: bool, f, *args) -> int:
-    """f(*args) with s as the current stream, and so its GPU as the current one: the library enqueues
-    there, and a GPU's default stream has the same handle as any other's."""
+def _call(here: bool, device, f, *args) -> int:
+    """f(*args) with `device` as the current GPU (here: it is): the library enqueues there, and a
+    GPU's default stream has the same handle as any other's."""
     if here:
         return f(*args)
-    with torch.cuda.stream(s):
+    with torch.cuda.device(device):
         return f(*args)
 
 
@@ -143,7 +140,7 @@ def qcache_tables(pages: int, block: int, held: torch.Tensor, new: torch.Tensor,
                           torch.empty(n, dtype=i32, device=dev),
                           torch.empty(4, dtype=torch.int64, device=dev))
     s, here = _use(stream, dev, held, new, free, table)
-    C.check(_call(s, here, C.lib().cm_qcache_tables,
+    C.check(_call(here, dev, C.lib().cm_qcache_tables,
                   pages, block, n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
                   table.data_ptr(), width, tokens, step.slots.data_ptr(), step.rows.data_ptr(),
                   step.lens.data_ptr(), step.info.data_ptr(), s.cuda_stream), "cm_qcache_tables")
@@ -190,9 +187,9 @@ def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
     if layers != v_layers:
         raise ValueError("k and v must have the same layers")
     s, here = _use(stream, cache.device, cache.codes, cache.scales, k, v, slots)
-    C.check(_call(s, here, C.lib().cm_qcache_write, ctypes.byref(cache.struct), layer, layers,
-                  _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens, slots.data_ptr(),
-                  s.cuda_stream), "cm_qcache_write")
+    C.check(_call(here, cache.device, C.lib().cm_qcache_write, ctypes.byref(cache.struct), layer,
+                  layers, _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens,
+                  slots.data_ptr(), s.cuda_stream), "cm_qcache_write")
 
 
 _WS: Dict[tuple, torch.Tensor] = {}
@@ -261,7 +258,8 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
     s, here = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
-    C.check(_call(s, here, _attention, cache, layer, step, s), "cm_qcache_attention")
+    with _made_on(None if stream is None and here else s):
+        C.check(_attention(cache, layer, step, s), "cm_qcache_attention")
     return out, lse
 
 

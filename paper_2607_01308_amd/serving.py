@@ -19,7 +19,7 @@ from typing import List, Optional, Sequence
 import torch
 
 from .binding import _DTYPES
-from .qcache import (QCache, QCacheStep, _call, _made_on, _use, check_rows, qcache_attention,
+from .qcache import (QCache, QCacheStep, _made_on, _use, check_rows, qcache_attention,
                      qcache_tables, qcache_write)
 
 
@@ -63,8 +63,11 @@ class ServingCache:
     def _refuse_capture(self, what: str, stream) -> None:
         if not self._held.is_cuda:
             return
-        if _call(*_use(stream, self._held.device), torch.cuda.is_current_stream_capturing):
-            raise RuntimeError(f"{what} cannot be captured into a graph: its replays would not move on")
+        s, here = _use(stream, self._held.device)
+        with _made_on(None if stream is None and here else s):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError(f"{what} cannot be captured into a graph: its replays would not "
+                                   "move on")
 
     def _pages(self, tokens: int) -> int:
         return -(-tokens // self.cache.B)
