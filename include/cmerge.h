@@ -25,6 +25,11 @@
  *   cm_qcache_tables        block tables and slots of a step from the lengths
  *   cm_qcache_write         K and V rows into a cache held in 8 bits on pages
  *   cm_qcache_attention     attention of a step's queries over that cache
+ * to decode with drafted tokens over it:
+ *   cm_norm_rotate          norms of queries and keys and the rotation for their positions
+ *   cm_verify_drafts        drafted tokens against the target's probabilities
+ *   cm_qcache_keep          the accepted tokens moved to the front, the others' pages freed
+ *   cm_qcache_copy          whole pages copied
  * and, to run step 1 without a second read of the fragments:
  *   cm_equal_key_mask       the deliveries whose digest the order needs
  *   cm_fragment_hash_select the Id of a subset of the deliveries
@@ -617,6 +622,121 @@ int32_t cm_qcache_attention_size(const cm_qcache* cache, const cm_qattention* st
 int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qattention* step,
                             void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------- drafted decoding
+ * What a model's layer does before its keys are written and its queries attend: the
+ * norm of each head and the rotation for the token's position (a drafted token's is not
+ * the place that it is written to).
+ *
+ * Heads of queries or of keys: head h of token t starts at element t * in_token_stride +
+ * h * in_head_stride of in_dev and holds d consecutive elements; its result goes to
+ * out_dev in the same way. 16-byte aligned, strides multiples of 16 bytes but for that of a
+ * dimension of size 1. out_dev may be in_dev with the same strides; else the two do not
+ * overlap. weight_dev: d elements of weight_dtype, or NULL: these heads are
+ * not normalised. heads 0 (or a NULL pointer to this): there are none. */
+typedef struct {
+  const void* in_dev;
+  int64_t in_token_stride;
+  int64_t in_head_stride;
+  void* out_dev;
+  int64_t out_token_stride;
+  int64_t out_head_stride;
+  const void* weight_dev;
+  int32_t weight_dtype;  /* cm_dtype */
+  int32_t heads;
+} cm_head_rows;
+
+/* For every token t and head row x of q and k:
+ *   y = x / sqrt(mean(x_0^2 .. x_{d-1}^2) + eps) * weight     (x itself without a weight)
+ *   pair i of y turned by the angle positions_dev[t] * base^(-2i/d): (a, b) becomes
+ *   (a cos - b sin, b cos + a sin); the pairs as rope->style says
+ * Angles are reduced in fp64, norms and products are in fp32, a result is rounded once to
+ * dtype (of the rows, cm_dtype). A row whose sum of squares leaves the range of fp32 gives
+ * zeros. positions_dev: n_tokens int32, any values. d is 64, 128 or 256. */
+int32_t cm_norm_rotate(int32_t d, int32_t dtype, int64_t n_tokens, const int32_t* positions_dev,
+                       const cm_rope* rope, float eps, const cm_head_rows* q, const cm_head_rows* k,
+                       void* stream);
+
+/* A step of drafted decoding. Request r brings the c nodes of the rows [rows_dev[r],
+ * rows_dev[r + 1]): a tree in which node 0 is the token that was sampled last and node i hangs
+ * on node parents_dev[i] < i of the request (-1 for node 0). Its nodes are its last c tokens: node i
+ * lies at place held + i of its pages, held = lens_dev[r] - c, and stands at position held + the
+ * number of its ancestors. A request has at most CM_DRAFT_MAX_NODES nodes.
+ *
+ * cm_verify_drafts decides which of them the target accepts. Row i of probs_dev holds the target's
+ * probabilities of the token after node i, drafts_dev[i] the node's token t_i, accept_dev[i] a number
+ * u_i in [0, 1), sample_dev[r] a number s in [0, 1). From node 0 on, the children x of a node are
+ * tried in order: with r the node's row of probs, m = 1 at first,
+ *   accepted if u_x * q(t_x) * m < r(t_x); otherwise r = max(r - m q, 0), m = sum r
+ * where q is the node's row of draft_probs, which its children were sampled from, independently
+ * of one another. Without draft_probs (NULL) a drafted token is taken as certain:
+ *   accepted if u_x * m < r(t_x); otherwise m -= r(t_x), r(t_x) = 0
+ * The first accepted child is the next node. Where there is none, tokens_dev[r] is the least v with
+ * r_0 + .. + r_v > s * sum r (the last v with r_v > 0 where s leaves none; where r holds nothing
+ * that of the node's row itself, -1 if that holds nothing either). Sums, products and comparisons
+ * are in fp64. A probability that is negative, infinite or NaN counts as 0, and so does that of a
+ * token outside [0, vocabulary).
+ * path_dev, at the request's rows: the numbers of the accepted nodes in order, 0 first, -1 behind
+ * them; counts_dev[r]: how many. A request without nodes, with more than CM_DRAFT_MAX_NODES, or whose
+ * rows do not lie in order in [0, n_rows] has count 0 and token -1; rows of no request are left as
+ * they are. A parent that is no earlier node of the request makes the node nobody's child. */
+#define CM_DRAFT_MAX_NODES 1024
+typedef struct {
+  int32_t n;                       /* requests, at most CM_QCACHE_MAX_REQUESTS */
+  int32_t dtype;                   /* cm_dtype of the probabilities */
+  int64_t n_rows;
+  int64_t vocabulary;
+  const void* probs_dev;           /* rows of `vocabulary` consecutive elements, */
+  int64_t probs_stride;            /* elements from one to the next */
+  const void* draft_probs_dev;     /* or NULL */
+  int64_t draft_probs_stride;
+  const int64_t* drafts_dev;       /* n_rows */
+  const int32_t* parents_dev;      /* n_rows */
+  const int32_t* rows_dev;         /* n + 1 */
+  const float* accept_dev;         /* n_rows */
+  const float* sample_dev;         /* n */
+  int32_t* path_dev;               /* n_rows */
+  int32_t* counts_dev;             /* n */
+  int64_t* tokens_dev;             /* n */
+} cm_drafts;
+int32_t cm_verify_drafts(const cm_drafts* drafts, void* stream);
+
+/* What a step leaves in the cache: of request r the first counts_dev[r] entries of path_dev at its
+ * rows are the nodes that stay, ascending. In every layer the K and V of node path[i] move from place
+ * held + path[i] to place held + i. A page that takes rows gets the greatest scale of the
+ * pages they come from and, where it holds rows before them, its own; codes are multiplied by
+ * old / new scale and rounded again. Nothing else is touched (rows behind the kept ones are left
+ * as they are). lens_out_dev[r] = held + counts; the pages of the table entries behind those,
+ * up to the last that lens had, are written to freed_dev (n_freed int32) in the order of the
+ * requests; the table is not changed. info_dev (2 int64): status, the pages freed.
+ * A row whose page or whose new place's page is not in [0, P) is not moved (in a page with such a row
+ * the page's own scale counts too). Lengths and pages go by
+ * counts alone (below 0 as 0, above the nodes as all of them); a request whose rows, length,
+ * counts or path are not as said has no rows moved and makes the status CM_EINVAL, and so does a
+ * freed_dev that is too short (info_dev[1] then holds the pages there are).
+ * 1 <= n <= CM_QCACHE_MAX_REQUESTS; info_dev is 8-byte aligned, the others 4-byte. What is written
+ * overlaps nothing that is read; no page that rows move in belongs to two requests. */
+typedef struct {
+  int32_t n;
+  int64_t n_rows;
+  const int32_t* table_dev;        /* n rows of table_width */
+  int64_t table_width;
+  const int32_t* lens_dev;         /* n */
+  const int32_t* rows_dev;         /* n + 1 */
+  const int32_t* path_dev;         /* n_rows */
+  const int32_t* counts_dev;       /* n */
+  int32_t* lens_out_dev;           /* n */
+  int32_t* freed_dev;
+  int64_t n_freed;
+  int64_t* info_dev;
+} cm_qkeep;
+int32_t cm_qcache_keep(const cm_qcache* cache, const cm_qkeep* step, void* stream);
+
+/* Copies pages src_dev[i] to dst_dev[i], i < n, codes and scales, in layers [first_layer,
+ * first_layer + n_layers). A pair with a page that is not in [0, P) is skipped. No destination
+ * is another one, nor a source (but its own). */
+int32_t cm_qcache_copy(const cm_qcache* cache, int32_t first_layer, int32_t n_layers, int64_t n,
+                       const int32_t* src_dev, const int32_t* dst_dev, void* stream);
+
 /* ---------------------------------------------------------------- timing
  * Optional per-kernel timing with HIP events recorded on the launch stream
  * around every kernel this library enqueues (off by default; a process-wide
@@ -625,7 +745,7 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
  * for one kernel name ("hash_prep", "hash_leaf", "hash_parent", "hash_final",
  * "knorm_rows", "knorm_tree", "order", "key_mask", "render_prep", "render",
  * "render_hash", "paged", "paged_hash_render", "qcache_tables", "qcache_write",
- * "qcache_attention"). "hash_parent" is the trees above the
+ * "qcache_attention", "norm_rotate", "verify_drafts", "qcache_keep", "qcache_copy"). "hash_parent" is the trees above the
  * stripes that the chunk kernels fold, with the Ids where one launch makes both and
  * where tensors of 2 to 64 chunks leave only the Ids to make; "hash_final" the Ids
  * otherwise. "key_mask" includes the comparison of re-deliveries. */

@@ -37,6 +37,14 @@ from .binding import (  # noqa: F401
     timing_reset,
     workspace_size,
 )
+from .drafting import (  # noqa: F401
+    QCacheKept,
+    Verified,
+    norm_rotate,
+    qcache_copy,
+    qcache_keep,
+    verify_drafts,
+)
 from .fragset import (  # noqa: F401
     LatentFragmentSet,
     MergedCache,

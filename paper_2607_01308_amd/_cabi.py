@@ -24,6 +24,7 @@ CM_ROPE_HALF = 0
 CM_ROPE_INTERLEAVED = 1
 CM_MAX_FRAGMENTS = 1024
 CM_QCACHE_MAX_REQUESTS = 1024
+CM_DRAFT_MAX_NODES = 1024
 NOALLOC_SCRATCH_BYTES = 64 << 20     # CM_NOALLOC_SCRATCH_BYTES
 
 PLAN_STATUS, PLAN_N, PLAN_NUNIQUE, PLAN_TOUT, PLAN_HEADER = 0, 1, 2, 3, 4
@@ -39,6 +40,7 @@ EXPORTS = (
     "cm_paged_workspace_size", "cm_paged_order", "cm_paged_hash_select", "cm_paged_tables",
     "cm_paged_render", "cm_paged_render_hash", "cm_paged_deliveries",
     "cm_qcache_tables", "cm_qcache_write", "cm_qcache_attention_size", "cm_qcache_attention",
+    "cm_norm_rotate", "cm_verify_drafts", "cm_qcache_keep", "cm_qcache_copy",
     "cm_timing_enable", "cm_timing_reset", "cm_timing_query",
 )
 
@@ -122,6 +124,58 @@ class CmQattention(ctypes.Structure):
     ]
 
 
+class CmHeadRows(ctypes.Structure):
+    _fields_ = [
+        ("in_dev", ctypes.c_void_p),
+        ("in_token_stride", ctypes.c_int64),
+        ("in_head_stride", ctypes.c_int64),
+        ("out_dev", ctypes.c_void_p),
+        ("out_token_stride", ctypes.c_int64),
+        ("out_head_stride", ctypes.c_int64),
+        ("weight_dev", ctypes.c_void_p),
+        ("weight_dtype", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+    ]
+
+
+class CmDrafts(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("n_rows", ctypes.c_int64),
+        ("vocabulary", ctypes.c_int64),
+        ("probs_dev", ctypes.c_void_p),
+        ("probs_stride", ctypes.c_int64),
+        ("draft_probs_dev", ctypes.c_void_p),
+        ("draft_probs_stride", ctypes.c_int64),
+        ("drafts_dev", ctypes.c_void_p),
+        ("parents_dev", ctypes.c_void_p),
+        ("rows_dev", ctypes.c_void_p),
+        ("accept_dev", ctypes.c_void_p),
+        ("sample_dev", ctypes.c_void_p),
+        ("path_dev", ctypes.c_void_p),
+        ("counts_dev", ctypes.c_void_p),
+        ("tokens_dev", ctypes.c_void_p),
+    ]
+
+
+class CmQkeep(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int32),
+        ("n_rows", ctypes.c_int64),
+        ("table_dev", ctypes.c_void_p),
+        ("table_width", ctypes.c_int64),
+        ("lens_dev", ctypes.c_void_p),
+        ("rows_dev", ctypes.c_void_p),
+        ("path_dev", ctypes.c_void_p),
+        ("counts_dev", ctypes.c_void_p),
+        ("lens_out_dev", ctypes.c_void_p),
+        ("freed_dev", ctypes.c_void_p),
+        ("n_freed", ctypes.c_int64),
+        ("info_dev", ctypes.c_void_p),
+    ]
+
+
 class CmError(RuntimeError):
     def __init__(self, status: int, where: str, message: str):
         self.status = status
@@ -143,6 +197,7 @@ def lib() -> ctypes.CDLL:
         FS = ctypes.POINTER(CmFragset)
         PS = ctypes.POINTER(CmPagedset)
         QC, QR, QA = (ctypes.POINTER(t) for t in (CmQcache, CmQrows, CmQattention))
+        HR = ctypes.POINTER(CmHeadRows)
         sig = {
             "cm_version": (I32, []),
             "cm_last_error": (ctypes.c_char_p, []),
@@ -185,6 +240,11 @@ def lib() -> ctypes.CDLL:
             "cm_qcache_write": (I32, [QC, I32, I32, I32, QR, QR, I64, P, P]),
             "cm_qcache_attention_size": (I32, [QC, QA, ctypes.POINTER(SZ)]),
             "cm_qcache_attention": (I32, [QC, I32, QA, P, SZ, P]),
+            "cm_norm_rotate": (I32, [I32, I32, I64, P, ctypes.POINTER(CmRope), ctypes.c_float, HR, HR,
+                                     P]),
+            "cm_verify_drafts": (I32, [ctypes.POINTER(CmDrafts), P]),
+            "cm_qcache_keep": (I32, [QC, ctypes.POINTER(CmQkeep), P]),
+            "cm_qcache_copy": (I32, [QC, I32, I32, I64, P, P, P]),
             "cm_timing_enable": (I32, [I32]),
             "cm_timing_reset": (I32, []),
             "cm_timing_query": (I32, [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),

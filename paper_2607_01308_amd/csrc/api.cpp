@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "cmerge.h"
+#include "draft.h"
 #include "internal.h"
 #include "qcache.h"
 
@@ -142,7 +143,8 @@ int64_t min_T(const cm::SetDesc& s) {
 const char* const kKernelNames[cm::K_COUNT] = {
     "hash_prep", "hash_leaf", "hash_parent", "hash_final", "knorm_rows", "knorm_tree",
     "order",     "key_mask",  "render_prep", "render",     "render_hash", "paged",
-    "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention"};
+    "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention", "norm_rotate",
+    "verify_drafts", "qcache_keep", "qcache_copy"};
 std::atomic<bool> g_timing{false};
 // set while this thread captures a call into a graph: no timing events then
 thread_local bool t_capturing = false;
@@ -1232,6 +1234,16 @@ int32_t element_bytes(int32_t dtype, int32_t* out) {
   return CM_OK;
 }
 
+struct Range {
+  const void* at;
+  int64_t bytes;
+  const char* name;
+};
+bool overlap(const Range& x, const Range& y) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+  return a < b + (uintptr_t)y.bytes && b < a + (uintptr_t)x.bytes;
+}
+
 // Strided rows that the kernels load in 16-byte pieces. The stride of a dimension of size 1 is
 // not used, and a caller's may be anything.
 struct Stride {
@@ -1304,22 +1316,14 @@ int32_t cm_qcache_tables(int64_t pages, int32_t block, int32_t n, const int32_t*
     return fail(CM_EINVAL, "rows_dev / lens_dev NULL or misaligned");
   if (!info_dev || !aligned(info_dev, 8)) return fail(CM_EINVAL, "info_dev is NULL or misaligned");
   // every workgroup reads the lengths and the free list, some after others have written
-  struct Range {
-    const void* at;
-    int64_t bytes;
-    const char* name;
-  };
   const Range read[] = {{held_dev, 4ll * n, "held_dev"}, {new_dev, 4ll * n, "new_dev"},
                         {free_dev, 4 * n_free, "free_dev"}};
   const Range written[] = {{table_dev, 4 * n * table_width, "table_dev"}, {slots_dev, 8 * n_tokens, "slots_dev"},
                            {rows_dev, 4ll * (n + 1), "rows_dev"}, {lens_dev, 4ll * n, "lens_dev"},
                            {info_dev, 32, "info_dev"}};
   for (const Range& w : written)
-    for (const Range& r : read) {
-      const uintptr_t a = reinterpret_cast<uintptr_t>(w.at), b = reinterpret_cast<uintptr_t>(r.at);
-      if (a < b + (uintptr_t)r.bytes && b < a + (uintptr_t)w.bytes)
-        return fail(CM_EINVAL, std::string(w.name) + " overlaps " + r.name);
-    }
+    for (const Range& r : read)
+      if (overlap(w, r)) return fail(CM_EINVAL, std::string(w.name) + " overlaps " + r.name);
   hipError_t e = cm::launch_qcache_tables(pages, __builtin_ctz((unsigned)block), n, held_dev,
                                           new_dev, free_dev, n_free, table_dev, table_width,
                                           n_tokens, slots_dev, rows_dev, lens_dev, info_dev,
@@ -1445,6 +1449,192 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
   a.few_count = reinterpret_cast<int32_t*>(ws);
   hipError_t e = cm::launch_qcache_attention(a, c.d, step->dtype, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_attention");
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------ drafted decoding
+namespace {
+
+int32_t check_head_rows(const char* what, const cm_head_rows* r, int64_t n_tokens, int32_t esize,
+                        cm::HeadRows* out) {
+  *out = cm::HeadRows{};
+  if (!r || r->heads == 0) return CM_OK;
+  const std::string name(what);
+  if (r->heads < 0 || r->heads > 65535) return fail(CM_ESHAPE, name + ".heads must be in [0, 65535]");
+  int32_t st = CM_OK, wsize = 4;
+  if (r->weight_dev) {
+    if ((st = element_bytes(r->weight_dtype, &wsize)) != CM_OK) return st;
+    if (!aligned(r->weight_dev, wsize)) return fail(CM_EINVAL, name + ".weight_dev is misaligned");
+  }
+  if (n_tokens == 0) return CM_OK;
+  if ((st = check_strides((name + ".in_dev").c_str(), r->in_dev, esize,
+                          {{n_tokens, r->in_token_stride}, {r->heads, r->in_head_stride}})) != CM_OK)
+    return st;
+  if ((st = check_strides((name + ".out_dev").c_str(), r->out_dev, esize,
+                          {{n_tokens, r->out_token_stride}, {r->heads, r->out_head_stride}})) != CM_OK)
+    return st;
+  out->in = static_cast<const uint8_t*>(r->in_dev);
+  out->out = static_cast<uint8_t*>(r->out_dev);
+  out->in_token = r->in_token_stride * esize;
+  out->in_head = r->in_head_stride * esize;
+  out->out_token = r->out_token_stride * esize;
+  out->out_head = r->out_head_stride * esize;
+  out->weight = r->weight_dev;
+  out->weight_dtype = r->weight_dtype;
+  out->heads = r->heads;
+  return CM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t cm_norm_rotate(int32_t d, int32_t dtype, int64_t n_tokens, const int32_t* positions_dev,
+                       const cm_rope* rope, float eps, const cm_head_rows* q, const cm_head_rows* k,
+                       void* stream) {
+  g_err.clear();
+  int32_t st = check_rope(rope), esize = 0;
+  if (st != CM_OK) return st;
+  if (d != 64 && d != 128 && d != 256)
+    return fail(CM_ESHAPE, "d must be 64, 128 or 256, got " + std::to_string(d));
+  if ((st = element_bytes(dtype, &esize)) != CM_OK) return st;
+  if (n_tokens < 0 || n_tokens > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_tokens must be in [0, 2^31), got " + std::to_string(n_tokens));
+  if (!std::isfinite(eps) || eps < 0.f) return fail(CM_EINVAL, "eps must be finite and >= 0");
+  cm::RotateArgs a;
+  if ((st = check_head_rows("q", q, n_tokens, esize, &a.q)) != CM_OK) return st;
+  if ((st = check_head_rows("k", k, n_tokens, esize, &a.k)) != CM_OK) return st;
+  if (n_tokens == 0 || a.q.heads + a.k.heads == 0) return CM_OK;
+  if (!positions_dev || !aligned(positions_dev, 4))
+    return fail(CM_EINVAL, "positions_dev is NULL or misaligned");
+  a.positions = positions_dev;
+  a.n_tokens = n_tokens;
+  a.log2_base = std::log2(rope->base);
+  a.eps = eps;
+  hipError_t e = cm::launch_norm_rotate(a, d, dtype, rope->style, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_norm_rotate");
+}
+
+int32_t cm_verify_drafts(const cm_drafts* s, void* stream) {
+  g_err.clear();
+  int32_t st = CM_OK, esize = 0;
+  if (!s) return fail(CM_EINVAL, "drafts is NULL");
+  if (s->n < 1 || s->n > CM_QCACHE_MAX_REQUESTS)
+    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
+                               "], got " + std::to_string(s->n));
+  if ((st = element_bytes(s->dtype, &esize)) != CM_OK) return st;
+  if (s->n_rows < 0 || s->n_rows > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_rows must be in [0, 2^31), got " + std::to_string(s->n_rows));
+  if (s->vocabulary < 1 || s->vocabulary > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "vocabulary must be in [1, 2^31), got " + std::to_string(s->vocabulary));
+  if (!s->rows_dev || !aligned(s->rows_dev, 4)) return fail(CM_EINVAL, "rows_dev is NULL or misaligned");
+  if (!s->counts_dev || !aligned(s->counts_dev, 4))
+    return fail(CM_EINVAL, "counts_dev is NULL or misaligned");
+  if (!s->tokens_dev || !aligned(s->tokens_dev, 8))
+    return fail(CM_EINVAL, "tokens_dev is NULL or misaligned");
+  if (!s->sample_dev || !aligned(s->sample_dev, 4))
+    return fail(CM_EINVAL, "sample_dev is NULL or misaligned");
+  if (s->n_rows > 0) {
+    if (!s->probs_dev || !aligned(s->probs_dev, esize))
+      return fail(CM_EINVAL, "probs_dev is NULL or misaligned");
+    if (s->draft_probs_dev && !aligned(s->draft_probs_dev, esize))
+      return fail(CM_EINVAL, "draft_probs_dev is misaligned");
+    for (int64_t stride : {s->probs_stride, s->draft_probs_dev ? s->draft_probs_stride : s->probs_stride})
+      if (s->n_rows > 1 && (stride < 0 || stride > ((int64_t)1 << 40)))
+        return fail(CM_EINVAL, "a row stride is negative or above 2^40");
+    if (!s->drafts_dev || !aligned(s->drafts_dev, 8))
+      return fail(CM_EINVAL, "drafts_dev is NULL or misaligned");
+    if (!s->parents_dev || !aligned(s->parents_dev, 4))
+      return fail(CM_EINVAL, "parents_dev is NULL or misaligned");
+    if (!s->accept_dev || !aligned(s->accept_dev, 4))
+      return fail(CM_EINVAL, "accept_dev is NULL or misaligned");
+    if (!s->path_dev || !aligned(s->path_dev, 4)) return fail(CM_EINVAL, "path_dev is NULL or misaligned");
+  }
+  cm::VerifyArgs a;
+  a.n = s->n;
+  a.n_rows = s->n_rows;
+  a.V = s->vocabulary;
+  a.p = s->probs_dev;
+  a.q = s->draft_probs_dev;
+  a.p_row = s->n_rows > 1 ? s->probs_stride : 0;
+  a.q_row = s->n_rows > 1 ? s->draft_probs_stride : 0;
+  a.drafts = s->drafts_dev;
+  a.parents = s->parents_dev;
+  a.rows = s->rows_dev;
+  a.accept = s->accept_dev;
+  a.sample = s->sample_dev;
+  a.path = s->path_dev;
+  a.counts = s->counts_dev;
+  a.tokens = s->tokens_dev;
+  hipError_t e = cm::launch_verify_drafts(a, s->dtype, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_verify_drafts");
+}
+
+int32_t cm_qcache_keep(const cm_qcache* cache, const cm_qkeep* s, void* stream) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c);
+  if (st != CM_OK) return st;
+  if (!s) return fail(CM_EINVAL, "step is NULL");
+  if (s->n < 1 || s->n > CM_QCACHE_MAX_REQUESTS)
+    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
+                               "], got " + std::to_string(s->n));
+  if (s->n_rows < 0 || s->n_rows > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_rows must be in [0, 2^31), got " + std::to_string(s->n_rows));
+  if (s->table_width < 1 || s->table_width > (((int64_t)1 << 30) >> c.b_shift))
+    return fail(CM_EINVAL, "table_width must be in [1, 2^30 / block], got " +
+                               std::to_string(s->table_width));
+  if (s->n_freed < 0 || s->n_freed > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_freed must be in [0, 2^31), got " + std::to_string(s->n_freed));
+  const int64_t n = s->n;
+  const Range read[] = {{s->table_dev, 4 * n * s->table_width, "table_dev"}, {s->lens_dev, 4 * n, "lens_dev"},
+                        {s->rows_dev, 4 * (n + 1), "rows_dev"}, {s->path_dev, 4 * s->n_rows, "path_dev"},
+                        {s->counts_dev, 4 * n, "counts_dev"}};
+  const Range written[] = {{s->lens_out_dev, 4 * n, "lens_out_dev"}, {s->freed_dev, 4 * s->n_freed, "freed_dev"},
+                           {s->info_dev, 16, "info_dev"}};
+  for (const Range& r : read)
+    if (r.bytes > 0 && (!r.at || !aligned(r.at, 4)))
+      return fail(CM_EINVAL, std::string(r.name) + " is NULL or misaligned");
+  for (const Range& w : written) {
+    if (w.bytes > 0 && (!w.at || !aligned(w.at, w.at == s->info_dev ? 8 : 4)))
+      return fail(CM_EINVAL, std::string(w.name) + " is NULL or misaligned");
+    for (const Range& r : read)
+      if (overlap(w, r)) return fail(CM_EINVAL, std::string(w.name) + " overlaps " + r.name);
+  }
+  cm::KeepArgs a;
+  a.c = c;
+  a.n = s->n;
+  a.n_rows = s->n_rows;
+  a.table = s->table_dev;
+  a.width = s->table_width;
+  a.lens = s->lens_dev;
+  a.rows = s->rows_dev;
+  a.path = s->path_dev;
+  a.counts = s->counts_dev;
+  a.lens_out = s->lens_out_dev;
+  a.freed = s->freed_dev;
+  a.n_freed = s->n_freed;
+  a.info = s->info_dev;
+  hipError_t e = cm::launch_qcache_keep(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_keep");
+}
+
+int32_t cm_qcache_copy(const cm_qcache* cache, int32_t first_layer, int32_t n_layers, int64_t n,
+                       const int32_t* src_dev, const int32_t* dst_dev, void* stream) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c);
+  if (st != CM_OK) return st;
+  if (first_layer < 0 || n_layers < 0 || first_layer > c.L - n_layers)
+    return fail(CM_EINVAL, "layers [first_layer, first_layer + n_layers) must lie in [0, L)");
+  if (n < 0 || n > 0x7FFFFFFF) return fail(CM_EINVAL, "n must be in [0, 2^31), got " + std::to_string(n));
+  if (n == 0 || n_layers == 0) return CM_OK;
+  if (!src_dev || !dst_dev || !aligned(src_dev, 4) || !aligned(dst_dev, 4))
+    return fail(CM_EINVAL, "src_dev / dst_dev NULL or misaligned");
+  hipError_t e = cm::launch_qcache_copy(c, first_layer, n_layers, n, src_dev, dst_dev,
+                                        static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_copy");
 }
 
 int32_t cm_timing_enable(int32_t on) {

@@ -1,0 +1,69 @@
+// Internal interface of the operators for drafted decoding (norm_rotate.hip, draft_*.hip).
+#pragma once
+
+#include "qcache.h"
+
+namespace cm {
+
+// Heads of queries or of keys (cm_head_rows), strides in bytes; heads 0: none.
+struct HeadRows {
+  const uint8_t* in;
+  uint8_t* out;
+  int64_t in_token, in_head, out_token, out_head;
+  const void* weight;    // nullptr: not normalised
+  int32_t weight_dtype;  // cm_dtype
+  int32_t heads;
+};
+
+struct RotateArgs {
+  HeadRows q, k;
+  const int32_t* positions;
+  int64_t n_tokens;
+  double log2_base;
+  float eps;
+};
+
+hipError_t launch_norm_rotate(RotateArgs a, int32_t d, int32_t dtype, int32_t style,
+                              hipStream_t stream);
+
+// Pages src[i] to dst[i], i < n, of layers [first_layer, first_layer + n_layers).
+hipError_t launch_qcache_copy(const QCacheDesc& c, int32_t first_layer, int32_t n_layers, int64_t n,
+                              const int32_t* src, const int32_t* dst, hipStream_t stream);
+
+// cm_qcache_keep.
+struct KeepArgs {
+  QCacheDesc c;
+  int32_t n;
+  int64_t n_rows;
+  const int32_t* table;
+  int64_t width;
+  const int32_t* lens;
+  const int32_t* rows;
+  const int32_t* path;
+  const int32_t* counts;
+  int32_t* lens_out;
+  int32_t* freed;
+  int64_t n_freed;
+  int64_t* info;
+};
+hipError_t launch_qcache_keep(const KeepArgs& a, hipStream_t stream);
+
+// cm_verify_drafts; strides of probabilities in elements.
+struct VerifyArgs {
+  int32_t n;
+  int64_t n_rows, V;
+  const void* p;
+  const void* q;           // nullptr: the drafts were not sampled
+  int64_t p_row, q_row;
+  const int64_t* drafts;
+  const int32_t* parents;
+  const int32_t* rows;
+  const float* accept;
+  const float* sample;
+  int32_t* path;
+  int32_t* counts;
+  int64_t* tokens;
+};
+hipError_t launch_verify_drafts(const VerifyArgs& a, int32_t dtype, hipStream_t stream);
+
+}  // namespace cm

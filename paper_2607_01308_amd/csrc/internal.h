@@ -325,6 +325,10 @@ enum KernelId {
   K_QCACHE_TABLES,
   K_QCACHE_WRITE,
   K_QCACHE_ATTENTION,
+  K_NORM_ROTATE,
+  K_VERIFY_DRAFTS,
+  K_QCACHE_KEEP,
+  K_QCACHE_COPY,
   K_COUNT
 };
 

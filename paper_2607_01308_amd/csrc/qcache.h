@@ -11,8 +11,8 @@ struct QCacheDesc {
   int64_t pages;
   uint8_t* codes;
   float* scales;
-  int64_t slice_codes() const { return ((pages * H) << b_shift) * d; }  // of one (layer, K/V)
-  int64_t slice_scales() const { return pages * H; }
+  __host__ __device__ int64_t slice_codes() const { return ((pages * H) << b_shift) * d; }  // of one (layer, K/V)
+  __host__ __device__ int64_t slice_scales() const { return pages * H; }
 };
 
 // Rows of K or V of a step (cm_qrows), strides in bytes.

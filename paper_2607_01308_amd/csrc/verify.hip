@@ -1,0 +1,310 @@
+// Drafted tokens verified against the target's probabilities, from given random numbers
+// (cm_verify_drafts).
+//
+// A walk from a request's node 0: the children x of a node are tried in order. With the node's row
+// p and the row q of probabilities that its children were sampled from, child x of token t is
+// accepted if u q(t) m < r(t); r = p and m = 1 at first, and a rejection leaves
+// r' = max(r - m q, 0), m' = sum r'. Since max(max(a - b, 0) - c, 0) = max(a - (b + c), 0) for
+// b, c >= 0, r after any number of rejections is max(p - M q, 0) with M the sum of their m:
+// one number is all that is kept. Without q a drafted token counts as certain: a rejection takes it
+// out of r, and its probability off m. Where no child is accepted the next token is the first v with
+// r_0 + .. + r_v > s sum r. Sums and comparisons are in fp64: u q(t) is then exact, and sums of a
+// hundred thousand terms are off by 1e-14 of themselves, not by 1e-6, beside which the borders of
+// a sampled token lie close.
+//
+// One workgroup takes a request: its walk looks at single probabilities, and a pass over a
+// row sums r where a rejected child has a sibling after it or the token is to be sampled.
+#include "draft.h"
+#include "qcache_ops.h"
+
+namespace cm {
+
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / 64;
+constexpr int kVec = 8;              // elements of a lane's load
+constexpr int kStep = 64 * kVec;     // and of a wave's
+
+// What is not a probability counts as none.
+__device__ __forceinline__ double clean(float x) {
+  return x > 0.f && x < __builtin_inff() ? (double)x : 0.0;
+}
+
+template <int ES>
+__device__ __forceinline__ float element(const void* row, int64_t v) {
+  if constexpr (ES == 4) return *(global_ptr<float>(row) + v);
+  else return __uint_as_float((uint32_t) * (global_ptr<uint16_t>(row) + v) << 16);
+}
+
+// kVec elements from v on; what lies behind V is 0. Rows begin at any element.
+typedef uint32_t words_f32 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t words_bf16 __attribute__((ext_vector_type(4), aligned(2)));
+template <int ES>
+__device__ __forceinline__ void load(const void* row, int64_t v, int64_t V, float (&x)[kVec]) {
+  if (v + kVec <= V) {
+    if constexpr (ES == 4) {
+      const CM_GLOBAL float* at = global_ptr<float>(row) + v;
+      const words_f32 a = *(const CM_GLOBAL words_f32*)at, b = *(const CM_GLOBAL words_f32*)(at + 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[k] = __uint_as_float(a[k]);
+        x[4 + k] = __uint_as_float(b[k]);
+      }
+    } else {
+      const words_bf16 a = *(const CM_GLOBAL words_bf16*)(global_ptr<uint16_t>(row) + v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        x[2 * k] = low_bf16(a[k]);
+        x[2 * k + 1] = high_bf16(a[k]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) x[k] = v + k < V ? element<ES>(row, v + k) : 0.f;
+  }
+}
+
+struct VerifyShared {
+  double part[kWaves];                 // sums of the waves' parts of the row
+  double sub[kWaves];                  // and of their steps
+  int64_t hit[kWaves], any[kWaves];
+  int64_t gone[CM_DRAFT_MAX_NODES];    // tokens taken out of r
+  int32_t n_gone;
+};
+
+template <int ES>
+__global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
+  __shared__ VerifyShared lds;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int req = blockIdx.x;
+  const int64_t first = a.rows[req], next = a.rows[req + 1];
+  const bool fits = first >= 0 && next >= first && next <= a.n_rows;
+  const int c = fits && next - first <= CM_DRAFT_MAX_NODES ? (int)(next - first) : 0;
+  if (c == 0) {
+    if (threadIdx.x == 0) {
+      a.counts[req] = 0;
+      a.tokens[req] = -1;
+    }
+    if (fits)
+      for (int64_t i = first + threadIdx.x; i < next; i += kThreads) a.path[i] = -1;
+    return;
+  }
+  const int32_t* parents = a.parents + first;
+  const int64_t* drafts = a.drafts + first;
+  const float* accept = a.accept + first;
+  int32_t* path = a.path + first;
+
+  // The next child of node `of` after node `after`, c where there is none. (All waves look.)
+  const auto child = [&](int of, int after) {
+    for (int i0 = after + 1; i0 < c; i0 += 64) {
+      const int i = i0 + lane;
+      const uint64_t hit = __ballot(i < c && parents[i] == of);
+      if (hit) return i0 + __builtin_ctzll(hit);
+    }
+    return c;
+  };
+  // Whether one of the children of `of` up to node `end` has token t.
+  const auto tried = [&](int of, int end, int64_t t) {
+    for (int i0 = of + 1; i0 < end; i0 += 64) {
+      const int i = i0 + lane;
+      if (__any(i < end && parents[i] == of && drafts[i] == t)) return true;
+    }
+    return false;
+  };
+
+  int node = 0, count = 0;
+  const uint8_t *p = nullptr, *q = nullptr;
+  const int64_t V = a.V;
+  const bool sampled = a.q != nullptr;
+  // A wave's part of the row: whole steps.
+  const int64_t part = ((V + kWaves - 1) / kWaves + kStep - 1) / kStep * kStep;
+
+  // r of the kVec elements from v on
+  const auto rest = [&](int64_t v, double M, double (&r)[kVec]) {
+    float x[kVec];
+    load<ES>(p, v, V, x);
+    if (sampled) {
+      float y[kVec];
+      load<ES>(q, v, V, y);
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) r[k] = fmax(fma(-M, clean(y[k]), clean(x[k])), 0.0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) r[k] = clean(x[k]);
+      const int gone = lds.n_gone;
+      for (int i = 0; i < gone; ++i) {
+        const int64_t t = lds.gone[i] - v;
+#pragma unroll
+        for (int k = 0; k < kVec; ++k) r[k] = t == k ? 0.0 : r[k];
+      }
+    }
+  };
+  const auto sum_of = [](const double (&r)[kVec]) {
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) s += r[k];
+    return s;
+  };
+  const auto wave_sum = [&](double x) {
+#pragma unroll
+    for (int by = 1; by < 64; by <<= 1) x += __shfl_xor(x, by);
+    return x;
+  };
+  // sum r over the row; the waves' parts stay in lds.part
+  const auto total = [&](double M) {
+    double s = 0.0;
+    const int64_t begin = wave * part, end = begin + part < V ? begin + part : V;
+    for (int64_t v = begin + lane * kVec; v < end; v += kStep) {
+      double r[kVec];
+      rest(v, M, r);
+      s += sum_of(r);
+    }
+    s = wave_sum(s);
+    __syncthreads();
+    if (lane == 0) lds.part[wave] = s;
+    __syncthreads();
+    double all = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all += lds.part[w];
+    return all;
+  };
+
+  double M = 0.0, m = 1.0;
+  if (threadIdx.x == 0) lds.n_gone = 0;
+  while (true) {
+    if (threadIdx.x == 0) path[count] = node;
+    ++count;
+    p = static_cast<const uint8_t*>(a.p) + (first + node) * a.p_row * ES;
+    if (sampled) q = static_cast<const uint8_t*>(a.q) + (first + node) * a.q_row * ES;
+    M = 0.0;
+    m = 1.0;
+    int x = child(node, node);
+    for (; x < c; x = child(node, x)) {
+      const int64_t t = drafts[x];
+      const bool in = t >= 0 && t < V;
+      const double pt = in ? clean(element<ES>(p, t)) : 0.0, u = accept[x];
+      double r, want = u;
+      if (sampled) {
+        const double qt = in ? clean(element<ES>(q, t)) : 0.0;
+        r = fmax(fma(-M, qt, pt), 0.0);
+        want *= qt;
+      } else {
+        r = tried(node, x, t) ? 0.0 : pt;
+      }
+      if (want * m < r) break;
+      if (sampled) {
+        M += m;
+        if (child(node, x) < c) m = total(M);    // (else the sum is made below)
+      } else {
+        m -= r;
+      }
+    }
+    if (x == c) break;
+    node = x;
+  }
+  for (int i = count + (int)threadIdx.x; i < c; i += kThreads) path[i] = -1;
+
+  // the token after `node`
+  if (!sampled) {
+    __syncthreads();
+    for (int i = node + 1 + (int)threadIdx.x; i < c; i += kThreads)
+      if (parents[i] == node) lds.gone[atomicAdd(&lds.n_gone, 1)] = drafts[i];
+    __syncthreads();
+  }
+  double all = total(M);
+  if (!(all > 0.0)) {                            // nothing is left: as if no child had been tried
+    M = 0.0;
+    __syncthreads();
+    if (threadIdx.x == 0) lds.n_gone = 0;
+    __syncthreads();
+    all = total(M);
+  }
+  const double want = (double)a.sample[req] * all;
+  // the first wave's part that passes it, else the last that holds anything
+  int w0 = -1;
+  double before = 0.0, run = 0.0, before_last = 0.0;
+  int last = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (lds.part[w] > 0.0) {
+      last = w;
+      before_last = run;
+    }
+    if (w0 < 0 && run + lds.part[w] > want) {
+      w0 = w;
+      before = run;
+    }
+    run += lds.part[w];
+  }
+  if (w0 < 0) {
+    w0 = last;
+    before = before_last;
+  }
+  // that part's steps, in order: each wave's sum of one step at a time
+  const int64_t begin = w0 * part, end = begin + part < V ? begin + part : V;
+  __syncthreads();
+  int64_t found = -1, final_one = -1;            // the token; the last one so far that has any
+  for (int64_t v0 = begin; v0 < end && found < 0; v0 += (int64_t)kWaves * kStep) {
+    const int64_t v = v0 + wave * kStep + lane * kVec;
+    double r[kVec];
+    if (v < end) rest(v, M, r);
+    else {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) r[k] = 0.0;
+    }
+    const double mine = sum_of(r);
+    double upto = mine;
+#pragma unroll
+    for (int by = 1; by < 64; by <<= 1) {
+      const double o = __shfl_up(upto, by);
+      if (lane >= by) upto += o;
+    }
+    if (lane == 63) lds.sub[wave] = upto;
+    __syncthreads();
+    double at = before;
+    for (int w = 0; w < wave; ++w) at += lds.sub[w];
+    at += upto - mine;
+    // the lane's first element that passes, and its last that has any
+    int hit = -1, any = -1;
+#pragma unroll
+    for (int k = 0; k < kVec; ++k) {
+      at += r[k];
+      if (r[k] > 0.0) any = k;
+      if (hit < 0 && r[k] > 0.0 && at > want) hit = k;
+    }
+    // the first lane of the first wave: through the LDS
+    const uint64_t hits = __ballot(hit >= 0), anys = __ballot(any >= 0);
+    if (lane == 0) {
+      lds.hit[wave] = -1;
+      lds.any[wave] = -1;
+    }
+    if (hits && lane == __builtin_ctzll(hits)) lds.hit[wave] = v + hit;
+    if (anys && lane == 63 - __builtin_clzll(anys)) lds.any[wave] = v + any;
+    __syncthreads();
+    for (int w = kWaves - 1; w >= 0; --w)
+      if (lds.hit[w] >= 0) found = lds.hit[w];
+    for (int w = 0; w < kWaves; ++w) {
+      if (lds.any[w] >= 0) final_one = lds.any[w];
+      before += lds.sub[w];
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    a.counts[req] = count;
+    a.tokens[req] = found >= 0 ? found : final_one;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_verify_drafts(const VerifyArgs& a, int32_t dtype, hipStream_t stream) {
+  ScopedTiming tm(K_VERIFY_DRAFTS, stream);
+  if (dtype == CM_BF16)
+    hipLaunchKernelGGL(verify_kernel<2>, dim3((uint32_t)a.n), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL(verify_kernel<4>, dim3((uint32_t)a.n), dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace cm
