@@ -27,6 +27,8 @@
  *   cm_qcache_attention     attention of a step's queries over that cache
  * to decode with drafted tokens over it:
  *   cm_norm_rotate          norms of queries and keys and the rotation for their positions
+ *   cm_qcache_tree          masks and positions of drafted nodes from their parents
+ *   cm_qcache_tree_attention  attention of the nodes' queries over the cache
  *   cm_verify_drafts        drafted tokens against the target's probabilities
  *   cm_qcache_keep          the accepted tokens moved to the front, the others' pages freed
  *   cm_qcache_copy          whole pages copied
@@ -660,9 +662,45 @@ int32_t cm_norm_rotate(int32_t d, int32_t dtype, int64_t n_tokens, const int32_t
  * rows_dev[r + 1]): a tree in which node 0 is the token that was sampled last and node i hangs
  * on node parents_dev[i] < i of the request (-1 for node 0). Its nodes are its last c tokens: node i
  * lies at place held + i of its pages, held = lens_dev[r] - c, and stands at position held + the
- * number of its ancestors. A request has at most CM_DRAFT_MAX_NODES nodes.
- *
- * cm_verify_drafts decides which of them the target accepts. Row i of probs_dev holds the target's
+ * number of its ancestors. A request has at most CM_DRAFT_MAX_NODES nodes. */
+#define CM_DRAFT_MAX_NODES 1024
+
+/* What the attention of such a step needs, once for all layers. masks_dev: words 64-bit words for each
+ * row; bit j % 64 of word j / 64 of node i's row is set for j = i and the ancestors j of i, with a
+ * window (above 0) for those less than window steps up alone. positions_dev: n_rows int32, the
+ * node's position. masks_dev NULL and words 0: positions alone. parents_dev NULL: chains, in which
+ * node i hangs on node i - 1; positions alone of any number of them (a prompt's). info_dev (n
+ * int32): a request's status. CM_EINVAL: its rows do not lie in order in [0, n_rows] (nothing is
+ * written for it), it has more nodes than CM_DRAFT_MAX_NODES or than its masks have bits (masks 0,
+ * positions lens - c), fewer tokens than nodes, or a parent that is neither -1 nor an earlier node
+ * (taken as -1). Rows of no request are left as they are.
+ * 1 <= n <= CM_QCACHE_MAX_REQUESTS, words at most CM_DRAFT_MAX_NODES / 64; masks_dev is 8-byte aligned,
+ * the others 4-byte. What is written overlaps nothing that is read. */
+int32_t cm_qcache_tree(int32_t n, int64_t n_rows, const int32_t* parents_dev, const int32_t* rows_dev,
+                       const int32_t* lens_dev, int32_t window, int32_t words, int64_t* masks_dev,
+                       int32_t* positions_dev, int32_t* info_dev, void* stream);
+
+/* Attention of the nodes' queries over one layer, as cm_qcache_attention but for what a row sees: of
+ * request r with c rows and lens tokens, row i sees place j < held = lens - c of the context (with a
+ * window: if j > positions - window, positions that of the row, in [held, held + c)) and the place
+ * held + j, 0 <= j < c, if bit j of its mask is set. Places whose table entry is not a page in
+ * [0, P) are hidden, and so are those below 0. Masks may be any, not only those of trees; a mask
+ * without bits leaves the context alone. Rows past max_rows are not computed; their nodes' K and V
+ * are seen by those whose masks say so. A request whose rows do not lie in order in [0, n_rows] has
+ * none. Workspace: cm_qcache_tree_attention_size() bytes, under the same rules as
+ * cm_qcache_attention's, whose workspace it may share. */
+typedef struct {
+  const int64_t* masks_dev;      /* n_rows * words */
+  int64_t words;                 /* 1 to CM_DRAFT_MAX_NODES / 64 */
+  const int32_t* positions_dev;  /* n_rows; not read without a window */
+} cm_qtree;
+int32_t cm_qcache_tree_attention_size(const cm_qcache* cache, const cm_qattention* step,
+                                      size_t* bytes_out);
+int32_t cm_qcache_tree_attention(const cm_qcache* cache, int32_t layer, const cm_qattention* step,
+                                 const cm_qtree* tree, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/* cm_verify_drafts decides which of them the target accepts. Row i of probs_dev holds the target's
  * probabilities of the token after node i, drafts_dev[i] the node's token t_i, accept_dev[i] a number
  * u_i in [0, 1), sample_dev[r] a number s in [0, 1). From node 0 on, the children x of a node are
  * tried in order: with r the node's row of probs, m = 1 at first,
@@ -679,7 +717,6 @@ int32_t cm_norm_rotate(int32_t d, int32_t dtype, int64_t n_tokens, const int32_t
  * them; counts_dev[r]: how many. A request without nodes, with more than CM_DRAFT_MAX_NODES, or whose
  * rows do not lie in order in [0, n_rows] has count 0 and token -1; rows of no request are left as
  * they are. A parent that is no earlier node of the request makes the node nobody's child. */
-#define CM_DRAFT_MAX_NODES 1024
 typedef struct {
   int32_t n;                       /* requests, at most CM_QCACHE_MAX_REQUESTS */
   int32_t dtype;                   /* cm_dtype of the probabilities */
@@ -745,7 +782,8 @@ int32_t cm_qcache_copy(const cm_qcache* cache, int32_t first_layer, int32_t n_la
  * for one kernel name ("hash_prep", "hash_leaf", "hash_parent", "hash_final",
  * "knorm_rows", "knorm_tree", "order", "key_mask", "render_prep", "render",
  * "render_hash", "paged", "paged_hash_render", "qcache_tables", "qcache_write",
- * "qcache_attention", "norm_rotate", "verify_drafts", "qcache_keep", "qcache_copy"). "hash_parent" is the trees above the
+ * "qcache_attention", "norm_rotate", "verify_drafts", "qcache_keep", "qcache_copy",
+ * "qcache_tree", "qcache_tree_attention"). "hash_parent" is the trees above the
  * stripes that the chunk kernels fold, with the Ids where one launch makes both and
  * where tensors of 2 to 64 chunks leave only the Ids to make; "hash_final" the Ids
  * otherwise. "key_mask" includes the comparison of re-deliveries. */

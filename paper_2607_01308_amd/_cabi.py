@@ -41,6 +41,7 @@ EXPORTS = (
     "cm_paged_render", "cm_paged_render_hash", "cm_paged_deliveries",
     "cm_qcache_tables", "cm_qcache_write", "cm_qcache_attention_size", "cm_qcache_attention",
     "cm_norm_rotate", "cm_verify_drafts", "cm_qcache_keep", "cm_qcache_copy",
+    "cm_qcache_tree", "cm_qcache_tree_attention_size", "cm_qcache_tree_attention",
     "cm_timing_enable", "cm_timing_reset", "cm_timing_query",
 )
 
@@ -135,6 +136,14 @@ class CmHeadRows(ctypes.Structure):
         ("weight_dev", ctypes.c_void_p),
         ("weight_dtype", ctypes.c_int32),
         ("heads", ctypes.c_int32),
+    ]
+
+
+class CmQtree(ctypes.Structure):
+    _fields_ = [
+        ("masks_dev", ctypes.c_void_p),
+        ("words", ctypes.c_int64),
+        ("positions_dev", ctypes.c_void_p),
     ]
 
 
@@ -242,6 +251,9 @@ def lib() -> ctypes.CDLL:
             "cm_qcache_attention": (I32, [QC, I32, QA, P, SZ, P]),
             "cm_norm_rotate": (I32, [I32, I32, I64, P, ctypes.POINTER(CmRope), ctypes.c_float, HR, HR,
                                      P]),
+            "cm_qcache_tree": (I32, [I32, I64, P, P, P, I32, I32, P, P, P, P]),
+            "cm_qcache_tree_attention_size": (I32, [QC, QA, ctypes.POINTER(SZ)]),
+            "cm_qcache_tree_attention": (I32, [QC, I32, QA, ctypes.POINTER(CmQtree), P, SZ, P]),
             "cm_verify_drafts": (I32, [ctypes.POINTER(CmDrafts), P]),
             "cm_qcache_keep": (I32, [QC, ctypes.POINTER(CmQkeep), P]),
             "cm_qcache_copy": (I32, [QC, I32, I32, I64, P, P, P]),

@@ -299,7 +299,8 @@ def timing_query(kernel: str):
 KERNELS = ("hash_prep", "hash_leaf", "hash_parent", "hash_final", "knorm_rows", "knorm_tree",
            "order", "key_mask", "render_prep", "render", "render_hash", "paged",
            "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention", "norm_rotate",
-           "verify_drafts", "qcache_keep", "qcache_copy")
+           "verify_drafts", "qcache_keep", "qcache_copy", "qcache_tree",
+           "qcache_tree_attention")
 
 
 class PagedSet:

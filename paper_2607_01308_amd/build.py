@@ -25,7 +25,8 @@ HOSTCHECK_LIB = os.path.join(ROOT, "tests", "native", "libcm_hostcheck.so")
 ARCH = "gfx950"
 SOURCES = ["api.cpp", "hash.hip", "knorm.hip", "norm_rotate.hip", "order.hip", "paged.hip",
            "qcache_attention.hip", "qcache_keep.hip", "qcache_prompt.hip", "qcache_tables.hip",
-           "qcache_write.hip", "render.hip", "render_hash.hip", "verify.hip"]
+           "qcache_tree.hip", "qcache_tree_fp32.hip", "qcache_write.hip", "render.hip", "render_hash.hip",
+           "verify.hip"]
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
           f"-I{INCLUDE}", f"-I{CSRC}"]
 DEVICE = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

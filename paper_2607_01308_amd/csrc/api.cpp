@@ -144,7 +144,7 @@ const char* const kKernelNames[cm::K_COUNT] = {
     "hash_prep", "hash_leaf", "hash_parent", "hash_final", "knorm_rows", "knorm_tree",
     "order",     "key_mask",  "render_prep", "render",     "render_hash", "paged",
     "paged_hash_render", "qcache_tables", "qcache_write", "qcache_attention", "norm_rotate",
-    "verify_drafts", "qcache_keep", "qcache_copy"};
+    "verify_drafts", "qcache_keep", "qcache_copy", "qcache_tree", "qcache_tree_attention"};
 std::atomic<bool> g_timing{false};
 // set while this thread captures a call into a graph: no timing events then
 thread_local bool t_capturing = false;
@@ -1278,6 +1278,69 @@ int32_t check_qattention_shape(const cm::QCacheDesc& c, const cm_qattention* s) 
   return CM_OK;
 }
 
+// The rest of it: first what a call without rows needs too.
+int32_t check_qattention(const cm_qattention* step) {
+  int32_t st = CM_OK, esize = 0;
+  if ((st = element_bytes(step->dtype, &esize)) != CM_OK) return st;
+  if (step->window < 0) return fail(CM_EINVAL, "window must be >= 0");
+  if (!std::isfinite(step->scale)) return fail(CM_EINVAL, "scale must be finite");
+  if (!step->rows_dev && step->n_rows != step->n)
+    return fail(CM_EINVAL, "without rows_dev there is one row for each request: n_rows == n");
+  if (step->rows_dev && !aligned(step->rows_dev, 4)) return fail(CM_EINVAL, "rows_dev is misaligned");
+  if (!step->lens_dev || !aligned(step->lens_dev, 4))
+    return fail(CM_EINVAL, "lens_dev is NULL or misaligned");
+  if (!step->table_dev || !aligned(step->table_dev, 4))
+    return fail(CM_EINVAL, "table_dev is NULL or misaligned");
+  return CM_OK;
+}
+
+int32_t check_qattention_rows(const cm_qattention* step) {
+  int32_t st = CM_OK;
+  const int32_t esize = step->dtype == CM_F32 ? 4 : 2;
+  if ((st = check_strides("q_dev", step->q_dev, esize,
+                          {{step->n_rows, step->q_row_stride}, {step->q_heads, step->q_head_stride}})) !=
+      CM_OK)
+    return st;
+  if ((st = check_strides("out_dev", step->out_dev, esize,
+                          {{step->n_rows, step->out_row_stride},
+                           {step->q_heads, step->out_head_stride}})) != CM_OK)
+    return st;
+  if (step->lse_dev && !aligned(step->lse_dev, 4)) return fail(CM_EINVAL, "lse_dev is misaligned");
+  return CM_OK;
+}
+
+// What the kernels read and write, but for how the work is cut.
+cm::QAttention qattention_of(const cm::QCacheDesc& c, int32_t layer, const cm_qattention* step) {
+  cm::QAttention a = {};
+  const int64_t codes = c.slice_codes(), scales = c.slice_scales();
+  a.kc = c.codes + 2 * (int64_t)layer * codes;
+  a.vc = a.kc + codes;
+  a.ks = c.scales + 2 * (int64_t)layer * scales;
+  a.vs = a.ks + scales;
+  a.pages = c.pages;
+  a.H = c.H;
+  a.G = step->q_heads / c.H;
+  a.b_shift = c.b_shift;
+  a.n = step->n;
+  a.q = step->q_dev;
+  a.q_row = step->q_row_stride;
+  a.q_head = step->q_head_stride;
+  a.out = step->out_dev;
+  a.out_row = step->out_row_stride;
+  a.out_head = step->out_head_stride;
+  a.lse = step->lse_dev;
+  a.rows = step->rows_dev;
+  a.lens = step->lens_dev;
+  a.table = step->table_dev;
+  a.width = step->table_width;
+  a.n_rows = step->n_rows;
+  a.max_rows = step->max_rows;
+  a.window = step->window;
+  a.scale_log2 = std::fabs(step->scale) * 1.4426950408889634f;
+  a.negate = step->scale < 0.f;
+  return a;
+}
+
 cm::QAttentionPlan qattention_plan(const cm::QCacheDesc& c, const cm_qattention* s) {
   return cm::plan_qcache_attention(c.H, c.d, s->q_heads / c.H, s->n, s->n_rows, s->max_rows,
                                    s->table_width << c.b_shift, s->dtype);
@@ -1379,63 +1442,20 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
                             void* workspace, size_t workspace_bytes, void* stream) {
   g_err.clear();
   cm::QCacheDesc c;
-  int32_t st = check_qcache(cache, &c), esize = 0;
+  int32_t st = check_qcache(cache, &c);
   if (st != CM_OK) return st;
   if (layer < 0 || layer >= c.L)
     return fail(CM_EINVAL, "layer must be in [0, L), got " + std::to_string(layer));
   if ((st = check_qattention_shape(c, step)) != CM_OK) return st;
-  if ((st = element_bytes(step->dtype, &esize)) != CM_OK) return st;
-  if (step->window < 0) return fail(CM_EINVAL, "window must be >= 0");
-  if (!std::isfinite(step->scale)) return fail(CM_EINVAL, "scale must be finite");
-  if (!step->rows_dev && step->n_rows != step->n)
-    return fail(CM_EINVAL, "without rows_dev there is one row for each request: n_rows == n");
-  if (step->rows_dev && !aligned(step->rows_dev, 4)) return fail(CM_EINVAL, "rows_dev is misaligned");
-  if (!step->lens_dev || !aligned(step->lens_dev, 4))
-    return fail(CM_EINVAL, "lens_dev is NULL or misaligned");
-  if (!step->table_dev || !aligned(step->table_dev, 4))
-    return fail(CM_EINVAL, "table_dev is NULL or misaligned");
+  if ((st = check_qattention(step)) != CM_OK) return st;
   if (step->n_rows == 0) return CM_OK;
-  if ((st = check_strides("q_dev", step->q_dev, esize,
-                          {{step->n_rows, step->q_row_stride}, {step->q_heads, step->q_head_stride}})) !=
-      CM_OK)
-    return st;
-  if ((st = check_strides("out_dev", step->out_dev, esize,
-                          {{step->n_rows, step->out_row_stride},
-                           {step->q_heads, step->out_head_stride}})) != CM_OK)
-    return st;
-  if (step->lse_dev && !aligned(step->lse_dev, 4)) return fail(CM_EINVAL, "lse_dev is misaligned");
+  if ((st = check_qattention_rows(step)) != CM_OK) return st;
   const cm::QAttentionPlan plan = qattention_plan(c, step);
   if (((int64_t)plan.few_max + 8) * c.H > 0x7FFFFFFF ||
       ((int64_t)plan.many_max + 8) * c.H > 0x7FFFFFFF)
     return fail(CM_ESHAPE, "too many query rows for one call");
   if ((st = check_ws(workspace, workspace_bytes, plan.bytes)) != CM_OK) return st;
-  cm::QAttention a;
-  const int64_t codes = c.slice_codes(), scales = c.slice_scales();
-  a.kc = c.codes + 2 * (int64_t)layer * codes;
-  a.vc = a.kc + codes;
-  a.ks = c.scales + 2 * (int64_t)layer * scales;
-  a.vs = a.ks + scales;
-  a.pages = c.pages;
-  a.H = c.H;
-  a.G = step->q_heads / c.H;
-  a.b_shift = c.b_shift;
-  a.n = step->n;
-  a.q = step->q_dev;
-  a.q_row = step->q_row_stride;
-  a.q_head = step->q_head_stride;
-  a.out = step->out_dev;
-  a.out_row = step->out_row_stride;
-  a.out_head = step->out_head_stride;
-  a.lse = step->lse_dev;
-  a.rows = step->rows_dev;
-  a.lens = step->lens_dev;
-  a.table = step->table_dev;
-  a.width = step->table_width;
-  a.n_rows = step->n_rows;
-  a.max_rows = step->max_rows;
-  a.window = step->window;
-  a.scale_log2 = std::fabs(step->scale) * 1.4426950408889634f;
-  a.negate = step->scale < 0.f;
+  cm::QAttention a = qattention_of(c, layer, step);
   a.few_unit = plan.few_unit;
   a.few_items = plan.few_items;
   a.few_max = plan.few_max;
@@ -1455,6 +1475,11 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
 
 // ------------------------------------------------------------------ drafted decoding
 namespace {
+
+cm::TreePlan tree_plan(const cm::QCacheDesc& c, const cm_qattention* s) {
+  return cm::plan_qcache_tree(c.H, c.d, s->q_heads / c.H, s->n, s->n_rows, s->max_rows,
+                              s->table_width << c.b_shift, s->dtype);
+}
 
 int32_t check_head_rows(const char* what, const cm_head_rows* r, int64_t n_tokens, int32_t esize,
                         cm::HeadRows* out) {
@@ -1514,6 +1539,91 @@ int32_t cm_norm_rotate(int32_t d, int32_t dtype, int64_t n_tokens, const int32_t
   a.eps = eps;
   hipError_t e = cm::launch_norm_rotate(a, d, dtype, rope->style, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_norm_rotate");
+}
+
+int32_t cm_qcache_tree(int32_t n, int64_t n_rows, const int32_t* parents_dev, const int32_t* rows_dev,
+                       const int32_t* lens_dev, int32_t window, int32_t words, int64_t* masks_dev,
+                       int32_t* positions_dev, int32_t* info_dev, void* stream) {
+  g_err.clear();
+  if (n < 1 || n > CM_QCACHE_MAX_REQUESTS)
+    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
+                               "], got " + std::to_string(n));
+  if (n_rows < 0 || n_rows > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_rows must be in [0, 2^31), got " + std::to_string(n_rows));
+  if (window < 0) return fail(CM_EINVAL, "window must be >= 0");
+  if (words < 0 || words > CM_DRAFT_MAX_NODES / 64 || (words == 0) != (masks_dev == nullptr))
+    return fail(CM_EINVAL, "words must be in [1, " + std::to_string(CM_DRAFT_MAX_NODES / 64) +
+                               "], or 0 and masks_dev NULL, got " + std::to_string(words));
+  if (!rows_dev || !lens_dev || !aligned(rows_dev, 4) || !aligned(lens_dev, 4))
+    return fail(CM_EINVAL, "rows_dev / lens_dev NULL or misaligned");
+  if (!aligned(parents_dev, 4)) return fail(CM_EINVAL, "parents_dev is misaligned");
+  if (!aligned(masks_dev, 8)) return fail(CM_EINVAL, "masks_dev is misaligned");
+  if (n_rows > 0 && (!positions_dev || !aligned(positions_dev, 4)))
+    return fail(CM_EINVAL, "positions_dev is NULL or misaligned");
+  if (!info_dev || !aligned(info_dev, 4)) return fail(CM_EINVAL, "info_dev is NULL or misaligned");
+  const Range read[] = {{parents_dev, parents_dev ? 4 * n_rows : 0, "parents_dev"}, {rows_dev, 4ll * (n + 1), "rows_dev"},
+                        {lens_dev, 4ll * n, "lens_dev"}};
+  const Range written[] = {{masks_dev, 8 * n_rows * words, "masks_dev"}, {positions_dev, 4 * n_rows, "positions_dev"},
+                           {info_dev, 4ll * n, "info_dev"}};
+  for (const Range& w : written)
+    for (const Range& r : read)
+      if (overlap(w, r)) return fail(CM_EINVAL, std::string(w.name) + " overlaps " + r.name);
+  hipError_t e = cm::launch_qcache_tree(n, n_rows, parents_dev, rows_dev, lens_dev, window, words,
+                                        reinterpret_cast<uint64_t*>(masks_dev), positions_dev, info_dev,
+                                        static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_tree");
+}
+
+int32_t cm_qcache_tree_attention_size(const cm_qcache* cache, const cm_qattention* step,
+                                      size_t* bytes_out) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c);
+  if (st != CM_OK) return st;
+  if ((st = check_qattention_shape(c, step)) != CM_OK) return st;
+  if (!bytes_out) return fail(CM_EINVAL, "bytes_out is NULL");
+  *bytes_out = tree_plan(c, step).bytes;
+  return CM_OK;
+}
+
+int32_t cm_qcache_tree_attention(const cm_qcache* cache, int32_t layer, const cm_qattention* step,
+                                 const cm_qtree* tree, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+  g_err.clear();
+  cm::QCacheDesc c;
+  int32_t st = check_qcache(cache, &c);
+  if (st != CM_OK) return st;
+  if (layer < 0 || layer >= c.L)
+    return fail(CM_EINVAL, "layer must be in [0, L), got " + std::to_string(layer));
+  if ((st = check_qattention_shape(c, step)) != CM_OK) return st;
+  if ((st = check_qattention(step)) != CM_OK) return st;
+  if (!tree) return fail(CM_EINVAL, "tree is NULL");
+  if (tree->words < 1 || tree->words > CM_DRAFT_MAX_NODES / 64)
+    return fail(CM_EINVAL, "words must be in [1, " + std::to_string(CM_DRAFT_MAX_NODES / 64) + "], got " +
+                               std::to_string(tree->words));
+  if (step->n_rows == 0) return CM_OK;
+  if ((st = check_qattention_rows(step)) != CM_OK) return st;
+  if (!tree->masks_dev || !aligned(tree->masks_dev, 8))
+    return fail(CM_EINVAL, "masks_dev is NULL or misaligned");
+  if (step->window > 0 && (!tree->positions_dev || !aligned(tree->positions_dev, 4)))
+    return fail(CM_EINVAL, "positions_dev is NULL or misaligned");
+  const cm::TreePlan plan = tree_plan(c, step);
+  if ((st = check_ws(workspace, workspace_bytes, plan.bytes)) != CM_OK) return st;
+  cm::TreeAttention a;
+  a.a = qattention_of(c, layer, step);
+  a.a.few_unit = plan.unit;
+  a.a.few_items = plan.items;
+  a.a.few_max = plan.places;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  a.a.few_part = reinterpret_cast<float*>(ws + plan.part_at);
+  a.a.few_count = reinterpret_cast<int32_t*>(ws);
+  a.masks = reinterpret_cast<const uint64_t*>(tree->masks_dev);
+  a.words = tree->words;
+  a.positions = tree->positions_dev;
+  a.least = plan.least;
+  hipError_t e = cm::launch_qcache_tree_attention(a, c.d, step->dtype, plan.tiles,
+                                                  static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_tree_attention");
 }
 
 int32_t cm_verify_drafts(const cm_drafts* s, void* stream) {

@@ -48,6 +48,31 @@ struct KeepArgs {
 };
 hipError_t launch_qcache_keep(const KeepArgs& a, hipStream_t stream);
 
+// Masks and positions of the nodes (cm_qcache_tree).
+hipError_t launch_qcache_tree(int32_t n, int64_t n_rows, const int32_t* parents, const int32_t* rows,
+                              const int32_t* lens, int64_t window, int32_t words, uint64_t* masks,
+                              int32_t* positions, int32_t* info, hipStream_t stream);
+
+// Tree attention: what it reads and writes beside the fields of QAttention that are not of requests of
+// many rows; few_items, few_max, few_unit, few_part and few_count are those of its plan.
+struct TreeAttention {
+  QAttention a;
+  const uint64_t* masks;
+  int64_t words;
+  const int32_t* positions;
+  int32_t least;           // units of a span at least
+};
+// How its work is cut, from what the host knows.
+struct TreePlan {
+  int32_t tiles;           // row tiles of 16 that a wave takes
+  int32_t unit, items, places, least;
+  size_t part_at, bytes;   // partial results in the workspace, its size
+};
+TreePlan plan_qcache_tree(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows, int32_t max_rows,
+                          int64_t longest, int32_t dtype);
+hipError_t launch_qcache_tree_attention(const TreeAttention& a, int32_t d, int32_t dtype, int32_t tiles,
+                                        hipStream_t stream);
+
 // cm_verify_drafts; strides of probabilities in elements.
 struct VerifyArgs {
   int32_t n;

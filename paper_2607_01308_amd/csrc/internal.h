@@ -329,6 +329,8 @@ enum KernelId {
   K_VERIFY_DRAFTS,
   K_QCACHE_KEEP,
   K_QCACHE_COPY,
+  K_QCACHE_TREE,
+  K_QCACHE_TREE_ATTENTION,
   K_COUNT
 };
 

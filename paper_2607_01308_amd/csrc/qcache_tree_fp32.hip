@@ -1,0 +1,11 @@
+// Tree attention (qcache_tree.h) for fp32 queries.
+#include "qcache_tree.h"
+
+namespace cm {
+
+hipError_t launch_tree_fp32(const TreeAttention& a, int32_t d, int32_t tiles, uint32_t groups,
+                            hipStream_t stream) {
+  return launch_tree<3>(a, d, tiles, groups, stream);
+}
+
+}  // namespace cm

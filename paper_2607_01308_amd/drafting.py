@@ -1,5 +1,6 @@
 """Decoding with drafted tokens over the 8-bit paged cache: the binding of cm_norm_rotate,
-cm_verify_drafts, cm_qcache_keep and cm_qcache_copy (include/cmerge.h).
+cm_qcache_tree, cm_qcache_tree_attention, cm_verify_drafts, cm_qcache_keep and
+cm_qcache_copy (include/cmerge.h). ServingCache (serving.py) strings them together.
 
 As in qcache.py, every call enqueues its work on one stream (the `stream` argument, else
 the current one), marks the tensors it was given as in use there and does not wait."""
@@ -14,7 +15,7 @@ import torch
 
 from . import _cabi as C
 from .binding import _DTYPES, _STYLES
-from .qcache import QCache, _call, _check, _made_on, _use
+from .qcache import QCache, _attention, _attention_step, _call, _check, _made_on, _use
 
 
 def _heads(x: torch.Tensor, out: Optional[torch.Tensor], weight: Optional[torch.Tensor], name: str,
@@ -74,6 +75,79 @@ def norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
                   ctypes.byref(rope), eps, ctypes.byref(qr), None if kr is None else ctypes.byref(kr),
                   s.cuda_stream), "cm_norm_rotate")
     return q_out, k_out
+
+
+@dataclass
+class QCacheTree:
+    """What the attention of a step of drafted nodes needs, on the device: masks [tokens, words] int64
+    (bit j % 64 of word j / 64: the row sees node j of its request), positions [tokens] int32, the
+    window that they were made for; info [n] int32: the requests' status."""
+    masks: Optional[torch.Tensor]
+    positions: torch.Tensor
+    window: int = 0
+    info: Optional[torch.Tensor] = None
+
+    def check(self) -> "QCacheTree":
+        """Waits for the step and raises if a request's rows, nodes or parents were not as they have
+        to be."""
+        if self.info is not None:
+            bad = [r for r, status in enumerate(self.info.tolist()) if status != C.CM_OK]
+            if bad:
+                raise C.CmError(C.CM_EINVAL, "cm_qcache_tree",
+                                f"requests {bad[:8]}: too many nodes or too few tokens, a parent that is "
+                                "no earlier node, or rows that do not lie in the step")
+        return self
+
+
+def qcache_tree(parents: Optional[torch.Tensor], rows: torch.Tensor, lens: torch.Tensor, tokens: int,
+                max_rows: int, window: int = 0, masks: bool = True, stream=None) -> QCacheTree:
+    """cm_qcache_tree: masks and positions of a step of `tokens` nodes, at most max_rows of a request.
+    parents [tokens] int32: the node that each hangs on, counted within its request, -1 for node 0
+    (None: chains); rows [n + 1], lens [n]: as qcache_tables gives them; window: positions that a node
+    sees, itself included (0: all); masks: False for positions alone."""
+    dev, n = lens.device, lens.numel()
+    if not lens.is_cuda:
+        raise ValueError("lens must live on a GPU")
+    _check(lens, "lens", torch.int32, dev, (n,))
+    _check(rows, "rows", torch.int32, dev, (n + 1,))
+    if parents is not None:
+        _check(parents, "parents", torch.int32, dev, (tokens,))
+    words = -(-max(max_rows, 1) // 64) if masks else 0
+    with _made_on(stream):
+        out = QCacheTree(torch.empty((tokens, words), dtype=torch.int64, device=dev) if masks else None,
+                         torch.empty(tokens, dtype=torch.int32, device=dev), window,
+                         torch.empty(n, dtype=torch.int32, device=dev))
+    s, here = _use(stream, dev, parents, rows, lens)
+    C.check(_call(here, dev, C.lib().cm_qcache_tree, n, tokens,
+                  None if parents is None else parents.data_ptr(), rows.data_ptr(), lens.data_ptr(), window,
+                  words, out.masks.data_ptr() if masks else None, out.positions.data_ptr(),
+                  out.info.data_ptr(), s.cuda_stream), "cm_qcache_tree")
+    return out
+
+
+def qcache_tree_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Tensor,
+                          lens: torch.Tensor, rows: Optional[torch.Tensor], tree: QCacheTree,
+                          max_rows: Optional[int] = None, scale: Optional[float] = None,
+                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                          stream=None):
+    """cm_qcache_tree_attention: queries q [rows, q_heads, d] of drafted nodes over one layer of the
+    cache; returns (out, lse). Each sees its request's context, the tokens before the nodes, and the
+    nodes that its mask has (tree.masks, with tree.positions where tree.window is not 0). Other
+    arguments as qcache_attention."""
+    dev, masks = cache.device, tree.masks
+    step, out, lse = _attention_step(cache, q, table, lens, rows, max_rows, scale, tree.window, out, lse,
+                                     stream)
+    if masks is None or masks.dim() != 2:
+        raise ValueError("tree.masks must be [rows, words]")
+    _check(masks, "tree.masks", torch.int64, dev, (q.shape[0], masks.shape[1]))
+    _check(tree.positions, "tree.positions", torch.int32, dev, (q.shape[0],))
+    of = C.CmQtree(masks.data_ptr(), masks.shape[1], tree.positions.data_ptr())
+    s, here = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, masks, tree.positions, out,
+                   lse)
+    with _made_on(None if stream is None and here else s):
+        C.check(_attention(cache, layer, step, s, "cm_qcache_tree_attention", (ctypes.byref(of),)),
+                "cm_qcache_tree_attention")
+    return out, lse
 
 
 @dataclass

@@ -196,11 +196,11 @@ _WS: Dict[tuple, torch.Tensor] = {}
 _NONE = torch.empty(0, dtype=torch.uint8)
 
 
-def _workspace(cache: QCache, step: C.CmQattention) -> torch.Tensor:
+def _workspace(cache: QCache, step: C.CmQattention, size: str) -> torch.Tensor:
     """Scratch for a call, allocated on the current stream."""
     need = ctypes.c_size_t(0)
-    C.check(C.lib().cm_qcache_attention_size(ctypes.byref(cache.struct), ctypes.byref(step),
-                                             ctypes.byref(need)), "cm_qcache_attention_size")
+    C.check(getattr(C.lib(), size)(ctypes.byref(cache.struct), ctypes.byref(step),
+                                   ctypes.byref(need)), size)
     ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
     # the calls count in it, and leave their counters at zero
     ws[:C.CM_QCACHE_COUNTER_BYTES].zero_()
@@ -211,19 +211,8 @@ def release_qcache_workspace() -> None:
     _WS.clear()
 
 
-def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Tensor,
-                     lens: torch.Tensor, rows: Optional[torch.Tensor] = None,
-                     max_rows: Optional[int] = None, scale: Optional[float] = None,
-                     window: int = 0, out: Optional[torch.Tensor] = None,
-                     lse: Optional[torch.Tensor] = None, stream=None):
-    """cm_qcache_attention: queries q [rows, q_heads, d] over one layer of the cache;
-    returns (out, lse). table [n, width], lens [n]: each request's pages and tokens, the
-    step's own included; rows [n + 1]: where each request's query rows begin (None: one
-    row for each request); max_rows: the most rows of a request (default: all of them,
-    or 1 without rows; the host does not see rows, so a decoding step that gives rows and
-    not max_rows goes the slower way of prompts); scale: of the scores (default
-    d ** -0.5); window: positions that a query sees, itself included (0: all up to its
-    own). out: q's shape and type; lse [rows, q_heads] float32 (made if not given)."""
+def _attention_step(cache: QCache, q, table, lens, rows, max_rows, scale, window, out, lse, stream):
+    """The checked arguments of an attention call as the library takes them, with out and lse."""
     dev = cache.device
     if q.dim() != 3 or q.shape[2] != cache.d:
         raise ValueError(f"q must be [rows, q_heads, {cache.d}], got {list(q.shape)}")
@@ -257,14 +246,33 @@ def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Te
         d ** -0.5 if scale is None else scale, q.data_ptr(), q.stride(0), q.stride(1),
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
-    s, here = _use(stream, dev, cache.codes, cache.scales, q, table, lens, rows, out, lse)
+    return step, out, lse
+
+
+def qcache_attention(cache: QCache, layer: int, q: torch.Tensor, table: torch.Tensor,
+                     lens: torch.Tensor, rows: Optional[torch.Tensor] = None,
+                     max_rows: Optional[int] = None, scale: Optional[float] = None,
+                     window: int = 0, out: Optional[torch.Tensor] = None,
+                     lse: Optional[torch.Tensor] = None, stream=None):
+    """cm_qcache_attention: queries q [rows, q_heads, d] over one layer of the cache;
+    returns (out, lse). table [n, width], lens [n]: each request's pages and tokens, the
+    step's own included; rows [n + 1]: where each request's query rows begin (None: one
+    row for each request); max_rows: the most rows of a request (default: all of them,
+    or 1 without rows; the host does not see rows, so a decoding step that gives rows and
+    not max_rows goes the slower way of prompts); scale: of the scores (default
+    d ** -0.5); window: positions that a query sees, itself included (0: all up to its
+    own). out: q's shape and type; lse [rows, q_heads] float32 (made if not given)."""
+    step, out, lse = _attention_step(cache, q, table, lens, rows, max_rows, scale, window, out, lse,
+                                     stream)
+    s, here = _use(stream, cache.device, cache.codes, cache.scales, q, table, lens, rows, out, lse)
     with _made_on(None if stream is None and here else s):
         C.check(_attention(cache, layer, step, s), "cm_qcache_attention")
     return out, lse
 
 
-def _attention(cache: QCache, layer: int, step: C.CmQattention, s) -> int:
-    """The call on s, which is the current stream.
+def _attention(cache: QCache, layer: int, step: C.CmQattention, s, call: str = "cm_qcache_attention",
+               more: tuple = ()) -> int:
+    """The call on s, which is the current stream; more: arguments of it after the step.
 
     Scratch is cached for (device, stream), so calls on two streams never share it, and
     replaced by a larger one where it is too small. A call that is being captured gets
@@ -272,11 +280,12 @@ def _attention(cache: QCache, layer: int, step: C.CmQattention, s) -> int:
     be replaced while the graph still refers to it."""
     capturing = torch.cuda.is_current_stream_capturing()
     key = (cache.device, s.cuda_stream)
-    ws = _workspace(cache, step) if capturing else _WS.get(key, _NONE)
-    args = ctypes.byref(cache.struct), layer, ctypes.byref(step)
-    f = C.lib().cm_qcache_attention
+    size = call + "_size"
+    ws = _workspace(cache, step, size) if capturing else _WS.get(key, _NONE)
+    args = ctypes.byref(cache.struct), layer, ctypes.byref(step), *more
+    f = getattr(C.lib(), call)
     status = f(*args, ws.data_ptr(), ws.numel(), s.cuda_stream)
     if status == C.CM_EWORKSPACE and not capturing:
-        ws = _WS[key] = _workspace(cache, step)
+        ws = _WS[key] = _workspace(cache, step, size)
         status = f(*args, ws.data_ptr(), ws.numel(), s.cuda_stream)
     return status

@@ -212,3 +212,19 @@ def attend(q, codes, scales, table, lens, rows, sees, positions, window=0, scale
                     A[a + i, j] = e @ vv.abs()
                     X[a + i, j] = (kk.abs() @ qq.abs()).max() * abs(scale)
     return out, lse, A, X
+
+
+def attend_bounds(dtype, d, T, out, A, X):
+    """(largest |error| of out, of lse) that the kernel's arithmetic allows, from its roundings.
+
+    A score is a sum of d products in fp32 (exact products, d additions, a factor and the running
+    exponent's subtraction): off by at most e = (d + 8) 2^-24 X. Weights and their sum then by
+    2 e + 2^-21 (an exp2 within two units, twice) + T 2^-24 for T additions, scaled by the joins of at most
+    some hundred parts (2^-17 in all). Weights enter as two bf16 terms for bf16 queries, the
+    rest after which is at most 2^-8 of 2^-8, as three for fp32 ones (2^-24); the output is
+    rounded once (2^-8, 2^-24)."""
+    e = (d + 8) * 2.0 ** -24 * X
+    p = (2 * e + 2.0 ** -21 + T * 2.0 ** -24 + 2.0 ** -17)[..., None]
+    w, r = (2.0 ** -16, 2.0 ** -8) if dtype == torch.bfloat16 else (2.0 ** -24, 2.0 ** -24)
+    off = (p + w) * A * 1.01
+    return off + r * (out.abs() + off) + 1e-30, e + 2.0 ** -17 + 2.0 ** -22 * X

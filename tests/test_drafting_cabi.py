@@ -148,8 +148,84 @@ def test_copies_refused(lib, first, layers, n, src, dst, code):
     assert lib.cm_qcache_copy(ref(cache()), first, layers, n, src, dst, None) == code
 
 
+def tree(lib, **over):
+    f = dict(n=2, n_rows=9, parents=0x100000, rows=0x110000, lens=0x120000, window=0, words=1,
+             masks=0x130000, positions=0x140000, info=0x150000)
+    f.update(over)
+    return lib.cm_qcache_tree(f["n"], f["n_rows"], f["parents"], f["rows"], f["lens"], f["window"],
+                              f["words"], f["masks"], f["positions"], f["info"], None)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(n=0), C.CM_EINVAL), (dict(n=C.CM_QCACHE_MAX_REQUESTS + 1), C.CM_EINVAL), (dict(n_rows=-1), C.CM_EINVAL),
+    (dict(n_rows=2 ** 31), C.CM_EINVAL), (dict(window=-1), C.CM_EINVAL), (dict(words=-1), C.CM_EINVAL),
+    (dict(words=0), C.CM_EINVAL), (dict(words=17), C.CM_EINVAL), (dict(masks=None), C.CM_EINVAL),
+    (dict(masks=0x130004), C.CM_EINVAL), (dict(parents=0x100002), C.CM_EINVAL), (dict(rows=None), C.CM_EINVAL),
+    (dict(rows=0x110001), C.CM_EINVAL), (dict(lens=None), C.CM_EINVAL), (dict(lens=0x120002), C.CM_EINVAL),
+    (dict(positions=None), C.CM_EINVAL), (dict(positions=0x140002), C.CM_EINVAL), (dict(info=None), C.CM_EINVAL),
+    (dict(info=0x150003), C.CM_EINVAL), (dict(positions=0x100010), C.CM_EINVAL), (dict(info=0x120004), C.CM_EINVAL),
+    (dict(masks=0x110000), C.CM_EINVAL),
+])
+def test_trees_refused(lib, over, code):
+    assert tree(lib, **over) == code
+    assert lib.cm_last_error().decode() != ""
+
+
+def step(**over):
+    f = dict(n=3, q_heads=8, dtype=C.CM_BF16, window=0, n_rows=12, max_rows=4, scale=0.1,
+             q_dev=0x300000, q_row_stride=1024, q_head_stride=128, out_dev=0x400000,
+             out_row_stride=1024, out_head_stride=128, lse_dev=0x500000, rows_dev=0x510000,
+             lens_dev=0x600000, table_dev=0x700000, table_width=9)
+    f.update(over)
+    return C.CmQattention(**f)
+
+
+def attend(lib, c=None, layer=0, ws=0x800000, bytes=1 << 40, tree=(0x900000, 1, 0xa00000), **over):
+    t = None if tree is None else ref(C.CmQtree(*tree))
+    return lib.cm_qcache_tree_attention(ref(c or cache()), layer, ref(step(**over)), t, ws, bytes, None)
+
+
+@pytest.mark.parametrize("over,code", [
+    (dict(n=0), C.CM_EINVAL), (dict(n=C.CM_QCACHE_MAX_REQUESTS + 1), C.CM_EINVAL), (dict(q_heads=6), C.CM_ESHAPE),
+    (dict(q_heads=65 * 4), C.CM_ESHAPE), (dict(dtype=2), C.CM_EDTYPE), (dict(window=-1), C.CM_EINVAL),
+    (dict(n_rows=-1), C.CM_EINVAL), (dict(n_rows=2 ** 31), C.CM_EINVAL), (dict(max_rows=-1), C.CM_EINVAL),
+    (dict(scale=float("nan")), C.CM_EINVAL), (dict(rows_dev=None), C.CM_EINVAL), (dict(rows_dev=0x510002), C.CM_EINVAL),
+    (dict(lens_dev=None), C.CM_EINVAL), (dict(table_dev=0x700002), C.CM_EINVAL), (dict(table_width=0), C.CM_EINVAL),
+    (dict(table_width=2 ** 27), C.CM_EINVAL), (dict(q_dev=0x300008), C.CM_EINVAL), (dict(q_row_stride=1025), C.CM_EINVAL),
+    (dict(out_dev=None), C.CM_EINVAL), (dict(out_head_stride=4), C.CM_EINVAL), (dict(lse_dev=0x500002), C.CM_EINVAL),
+    (dict(layer=-1), C.CM_EINVAL), (dict(layer=2), C.CM_EINVAL), (dict(tree=None), C.CM_EINVAL),
+    (dict(tree=(None, 1, 0xa00000)), C.CM_EINVAL), (dict(tree=(0x900004, 1, 0xa00000)), C.CM_EINVAL),
+    (dict(tree=(0x900000, 0, 0xa00000)), C.CM_EINVAL), (dict(tree=(0x900000, 17, 0xa00000)), C.CM_EINVAL),
+    (dict(window=5, tree=(0x900000, 1, None)), C.CM_EINVAL), (dict(window=5, tree=(0x900000, 1, 0xa00002)), C.CM_EINVAL),
+    (dict(ws=None), C.CM_EWORKSPACE), (dict(ws=0x800010), C.CM_EWORKSPACE), (dict(bytes=1000), C.CM_EWORKSPACE),
+])
+def test_tree_attention_refused(lib, over, code):
+    assert attend(lib, **over) == code
+    assert lib.cm_last_error().decode() != ""
+
+
+def test_tree_attention_sizes(lib):
+    def size(c, **over):
+        out = ctypes.c_size_t(0)
+        assert lib.cm_qcache_tree_attention_size(ref(c), ref(step(**over)), ref(out)) == C.CM_OK
+        return out.value
+
+    assert attend(lib, n_rows=0, q_dev=None, out_dev=None, ws=None) == C.CM_OK
+    assert lib.cm_qcache_tree_attention_size(ref(cache()), ref(step()), None) == C.CM_EINVAL
+    assert lib.cm_qcache_tree_attention_size(ref(cache()), None, ref(ctypes.c_size_t())) == C.CM_EINVAL
+    need = size(cache())
+    assert attend(lib, bytes=need - 1) == C.CM_EWORKSPACE
+    # partial results follow from the workgroups that run together, not from rows or lengths
+    most = max(size(cache(H=h, L=1), q_heads=h * 4, n_rows=r, max_rows=r, table_width=w)
+               for h in (1, 8, 64, 300) for r in (1, 4, 100, 100000) for w in (9, 1 << 20))
+    assert need < most < 256 << 20
+
+
 def test_binding_refusals():
     """By type, shape and device, without a GPU."""
+    lens = torch.tensor([3], dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU"):
+        cm.qcache_tree(None, torch.tensor([0, 3], dtype=torch.int32), lens, 3, 3)
     q = torch.zeros((3, 4, 64))
     pos = torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError, match="GPU"):
