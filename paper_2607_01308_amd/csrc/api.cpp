@@ -1551,7 +1551,7 @@ int32_t cm_qcache_tree(int32_t n, int64_t n_rows, const int32_t* parents_dev, co
   if (n_rows < 0 || n_rows > 0x7FFFFFFF)
     return fail(CM_EINVAL, "n_rows must be in [0, 2^31), got " + std::to_string(n_rows));
   if (window < 0) return fail(CM_EINVAL, "window must be >= 0");
-  if (words < 0 || words > CM_DRAFT_MAX_NODES / 64 || (words == 0) != (masks_dev == nullptr))
+  if (words < 0 || words > CM_DRAFT_MAX_NODES / 64 || (n_rows > 0 && (words == 0) != (masks_dev == nullptr)))
     return fail(CM_EINVAL, "words must be in [1, " + std::to_string(CM_DRAFT_MAX_NODES / 64) +
                                "], or 0 and masks_dev NULL, got " + std::to_string(words));
   if (!rows_dev || !lens_dev || !aligned(rows_dev, 4) || !aligned(lens_dev, 4))

@@ -1,5 +1,6 @@
 """ServingCache: requests served from an 8-bit paged cache, step after step. It strings
-qcache_tables, qcache_write and qcache_attention together and keeps what they need
+qcache_tables, qcache_write and qcache_attention together, and for drafted tokens
+qcache_tree, qcache_tree_attention, qcache_keep and qcache_copy, and keeps what they need
 between steps: the block table, the lengths and the free pages, on the device. The host
 follows with numbers alone, so no call waits for the device.
 
@@ -9,16 +10,28 @@ follows with numbers alone, so no call waits for the device.
     for layer in range(L):
         sc.write(layer, k, v, step)               # the new tokens' K and V, [tokens, H, d]
         out, lse = sc.attend(layer, q, step)      # their queries, [tokens, q_heads, d]
-    sc.release(0)                                 # its pages are free again"""
+    sc.release(0)                                 # its pages are free again
+
+A step of drafted tokens brings each place a tree, of which the target accepts a path:
+
+    sc.fork(0, 1)                                 # place 1 goes on from place 0's tokens
+    step = sc.draft([[-1, 0, 0, 1], [-1, 0], ...])           # each node's parent
+    q, k = norm_rotate(q, k, sc.positions(step), rope_base, q_weight=.., k_weight=..)
+    sc.write(layer, k, v, step)
+    out, lse = sc.attend(layer, q, step)
+    done = verify_drafts(probs, drafts, step.parents, step.tables.rows, accept, sample)
+    sc.accept(step, done.path, done.counts.tolist())         # the others' pages are free again"""
 
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
+from ._cabi import CM_DRAFT_MAX_NODES
 from .binding import _DTYPES
+from .drafting import QCacheTree, qcache_copy, qcache_keep, qcache_tree, qcache_tree_attention
 from .qcache import (QCache, QCacheStep, _made_on, _use, check_rows, qcache_attention,
                      qcache_tables, qcache_write)
 
@@ -27,10 +40,21 @@ from .qcache import (QCache, QCacheStep, _made_on, _use, check_rows, qcache_atte
 class ServingStep:
     """A step of ServingCache.extend: the new tokens of all places, place after place.
     tables: slots, rows and lengths on the device; tokens: how many; max_rows: the most of
-    one place."""
+    one place; new: how many of each. Of ServingCache.draft also the nodes' parents [tokens] int32 and
+    their tree, on the device."""
     tables: QCacheStep
     tokens: int
     max_rows: int
+    new: Tuple[int, ...] = ()
+    parents: Optional[torch.Tensor] = None
+    tree: Optional[QCacheTree] = None
+
+
+@dataclass
+class _Shared:
+    """Pages that several places hold, as consecutive entries of their tables."""
+    pages: int
+    places: int
 
 
 class ServingCache:
@@ -38,9 +62,9 @@ class ServingCache:
     `cache` (all of them: what they held is lost). Calls enqueue on one stream (`stream`,
     else the current one); a caller that changes streams between calls orders them.
 
-    The lengths and the free pages move on with each extend, load and release on the host, so
-    these are not captured into a HIP graph, whose replays would deal out the same pages
-    again; write and attend of a step may be."""
+    The lengths and the free pages move on with each extend, draft, accept, fork, load and
+    release on the host, so these are not captured into a HIP graph, whose replays would deal
+    out the same pages again; write, attend and positions of a step may be."""
 
     def __init__(self, cache: QCache, places: int, max_len: int):
         if places < 1 or max_len < 1:
@@ -55,6 +79,9 @@ class ServingCache:
         torch.arange(cache.P, dtype=i32, device=dev, out=self._free[:cache.P])
         self._head, self._tail = 0, cache.P
         self._new: Optional[tuple] = None                 # the last step's new lengths
+        self._parents: Optional[tuple] = None             # the last drafted step's parents
+        # what each place shares with others: the first entries of its table
+        self._shared: List[List[_Shared]] = [[] for _ in range(self.places)]
 
     @property
     def free_pages(self) -> int:
@@ -94,10 +121,116 @@ class ServingCache:
                                self.table, sum(new), stream)
         self._head += need
         self._held, self.lengths = tables.lens, after
-        return ServingStep(tables, sum(new), max(new))
+        return ServingStep(tables, sum(new), max(new), new)
+
+    def draft(self, parents: Sequence[Sequence[int]], window: int = 0, stream=None) -> ServingStep:
+        """Room for a tree of drafted tokens in each place r: parents[r][i] is the node that node i
+        hangs on, -1 for node 0, the token that was sampled last (no nodes: nothing for that
+        place). window: positions that a node sees, itself included (0: all). The step is refused, and
+        nothing changed, where extend would refuse it."""
+        self._refuse_capture("draft", stream)
+        parents = tuple(tuple(int(x) for x in tree) for tree in parents)
+        if len(parents) != self.places:
+            raise ValueError(f"parents must be of {self.places} places, got {len(parents)}")
+        for r, tree in enumerate(parents):
+            if len(tree) > CM_DRAFT_MAX_NODES:
+                raise ValueError(f"place {r} has {len(tree)} nodes, more than {CM_DRAFT_MAX_NODES}")
+            if any(not 0 <= p < i for i, p in enumerate(tree) if i) or tree[:1] not in ((), (-1,)):
+                raise ValueError(f"place {r}: node 0 hangs on -1, every other on an earlier one, got "
+                                 f"{list(tree)}")
+        if window < 0:
+            raise ValueError(f"window must be >= 0, got {window}")
+        step = self.extend([len(tree) for tree in parents], stream)
+        if self._parents is None or self._parents[0] != parents:
+            self._parents = (parents, *self._upload([p for tree in parents for p in tree], stream))
+        elif self._held.is_cuda:
+            _use(stream, self._held.device, self._parents[1])
+        step.parents = self._parents[1]
+        step.tree = qcache_tree(step.parents, step.tables.rows, step.tables.lens, step.tokens,
+                                step.max_rows, window, stream=stream)
+        return step
+
+    def _upload(self, numbers: Sequence[int], stream):
+        """The numbers as int32 on the device, and the host memory that they come from."""
+        with _made_on(stream):
+            host = torch.tensor(numbers, dtype=torch.int32, pin_memory=self._held.is_cuda)
+            return host.to(self._held.device, non_blocking=True), host
+
+    def positions(self, step: ServingStep, stream=None) -> torch.Tensor:
+        """The positions of a step's tokens [tokens] int32: of drafted ones those of their trees."""
+        if step.tree is not None:
+            return step.tree.positions
+        return qcache_tree(None, step.tables.rows, step.tables.lens, step.tokens, step.max_rows,
+                           masks=False, stream=stream).positions
+
+    def accept(self, step: ServingStep, path: torch.Tensor, counts: Sequence[int], stream=None) -> None:
+        """Of the nodes of a drafted step, the last one, the first counts[r] of place r's path (as
+        verify_drafts gives it) stay, and their K and V move to the front; the others' pages are
+        free again."""
+        self._refuse_capture("accept", stream)
+        counts = tuple(int(x) for x in counts)
+        if step.tables.lens is not self._held:
+            raise ValueError("accept is of the last step, and once; nothing may come between")
+        if len(counts) != self.places or any(not 0 <= k <= c for k, c in zip(counts, step.new)):
+            raise ValueError(f"counts must be of {self.places} places, each at most its nodes "
+                             f"{list(step.new)}, got {list(counts)}")
+        after = [a - c + k for a, c, k in zip(self.lengths, step.new, counts)]
+        pages = sum(self._pages(a) - self._pages(b) for a, b in zip(self.lengths, after))
+        if path.numel() != step.tokens:
+            raise ValueError(f"path must be [{step.tokens}], got {list(path.shape)}")
+        on_device, _host = self._upload(counts, stream)
+        self._room(pages, stream)
+        kept = qcache_keep(self.cache, self.table, step.tables.lens, step.tables.rows, path, on_device,
+                           self._free[self._tail:self._tail + pages], stream)
+        self._tail += pages
+        self._held, self.lengths = kept.lens, after
+
+    def fork(self, place: int, to: int, stream=None) -> None:
+        """The empty place `to` goes on from the tokens of `place`: both hold the same full pages,
+        which are free again when the last of their places is released, and `to` a copy of a page
+        that is not full."""
+        for x in (place, to):
+            if not 0 <= x < self.places:
+                raise ValueError(f"place must be in [0, {self.places}), got {x}")
+        if self.lengths[to] or to == place:
+            raise ValueError(f"place {to} is not empty")
+        self._refuse_capture("fork", stream)
+        full, part = divmod(self.lengths[place], self.cache.B)
+        if part and self.free_pages < 1:
+            raise RuntimeError("the fork needs a page, none is free")
+        if self._held.is_cuda:
+            _use(stream, self._held.device, self._free, self._held, self.table)
+        with _made_on(stream):
+            page = self._free[self._head:self._head + 1]
+            if part:
+                qcache_copy(self.cache, self.table[place, full:full + 1], page, stream=stream)
+                self.table[to, full:full + 1] = page
+            self.table[to, :full] = self.table[place, :full]
+            self._held = self._held.clone()               # (a step may still be read)
+            self._held[to] = self._held[place]
+        self._head += part > 0
+        own = full - sum(run.pages for run in self._shared[place])
+        if own:
+            self._shared[place].append(_Shared(own, 1))
+        for run in self._shared[place]:
+            run.places += 1
+        self._shared[to] = list(self._shared[place])
+        self.lengths[to] = self.lengths[place]
+
+    def _room(self, pages: int, stream) -> None:
+        """Room for `pages` more behind the free ones."""
+        if self._tail + pages <= self._free.numel():
+            return
+        if self._held.is_cuda:
+            _use(stream, self._held.device, self._free)
+        with _made_on(stream):
+            left = self._free[self._head:self._tail].clone()
+            self._free[:left.numel()] = left
+        self._head, self._tail = 0, left.numel()
 
     def release(self, place: int, stream=None) -> None:
-        """Empties a place; its pages are free again, after the work enqueued so far."""
+        """Empties a place; its pages are free again, after the work enqueued so far (what it shares
+        with other places when the last of them is released)."""
         if not 0 <= place < self.places:
             raise ValueError(f"place must be in [0, {self.places}), got {place}")
         self._refuse_capture("release", stream)
@@ -106,15 +239,22 @@ class ServingCache:
             return
         if self._held.is_cuda:
             _use(stream, self._held.device, self._free, self._held, self.table)
+        # the table's entries whose pages nobody else holds
+        runs, at = [], 0
+        for run in self._shared[place]:
+            run.places -= 1
+            if run.places == 0:
+                runs.append((at, at + run.pages))
+            at += run.pages
+        self._shared[place] = []
+        runs.append((at, pages))
+        self._room(pages, stream)
         with _made_on(stream):
-            if self._tail + pages > self._free.numel():
-                left = self._free[self._head:self._tail].clone()
-                self._free[:left.numel()] = left
-                self._head, self._tail = 0, left.numel()
-            self._free[self._tail:self._tail + pages] = self.table[place, :pages]
+            for a, b in runs:
+                self._free[self._tail:self._tail + b - a] = self.table[place, a:b]
+                self._tail += b - a
             self._held = self._held.clone()               # (a step may still be read)
             self._held[place:place + 1].zero_()
-        self._tail += pages
         self.lengths[place] = 0
 
     def write(self, layer: int, k: torch.Tensor, v: torch.Tensor, step: ServingStep,
@@ -128,7 +268,14 @@ class ServingCache:
                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                stream=None):
         """qcache_attention of the step's queries, [tokens, q_heads, d], each over its place's
-        tokens up to its own; returns (out, lse)."""
+        tokens up to its own; of a drafted step qcache_tree_attention, each over its place's tokens
+        before the step and its ancestors (the window is draft's); returns (out, lse)."""
+        if step.tree is not None:
+            if window not in (0, step.tree.window):
+                raise ValueError(f"the step was drafted for a window of {step.tree.window}, not {window}")
+            return qcache_tree_attention(self.cache, layer, q, self.table, step.tables.lens,
+                                         step.tables.rows, step.tree, max_rows=step.max_rows, scale=scale,
+                                         out=out, lse=lse, stream=stream)
         return qcache_attention(self.cache, layer, q, self.table, step.tables.lens,
                                 rows=step.tables.rows, max_rows=step.max_rows, scale=scale,
                                 window=window, out=out, lse=lse, stream=stream)
