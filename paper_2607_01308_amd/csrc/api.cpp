@@ -1616,7 +1616,7 @@ int32_t cm_qcache_tree_attention(const cm_qcache* cache, int32_t layer, const cm
   a.a.few_max = plan.places;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   a.a.few_part = reinterpret_cast<float*>(ws + plan.part_at);
-  a.a.few_count = reinterpret_cast<int32_t*>(ws);
+  a.a.many_found = ws + plan.cuts_at;
   a.masks = reinterpret_cast<const uint64_t*>(tree->masks_dev);
   a.words = tree->words;
   a.positions = tree->positions_dev;

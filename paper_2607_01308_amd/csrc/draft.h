@@ -54,7 +54,7 @@ hipError_t launch_qcache_tree(int32_t n, int64_t n_rows, const int32_t* parents,
                               int32_t* positions, int32_t* info, hipStream_t stream);
 
 // Tree attention: what it reads and writes beside the fields of QAttention that are not of requests of
-// many rows; few_items, few_max, few_unit, few_part and few_count are those of its plan.
+// many rows; few_items, few_max, few_unit, few_part and many_found are those of its plan.
 struct TreeAttention {
   QAttention a;
   const uint64_t* masks;
@@ -66,7 +66,7 @@ struct TreeAttention {
 struct TreePlan {
   int32_t tiles;           // row tiles of 16 that a wave takes
   int32_t unit, items, places, least;
-  size_t part_at, bytes;   // partial results in the workspace, its size
+  size_t cuts_at, part_at, bytes;  // which tiles are cut and partial results in the workspace, its size
 };
 TreePlan plan_qcache_tree(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_rows, int32_t max_rows,
                           int64_t longest, int32_t dtype);

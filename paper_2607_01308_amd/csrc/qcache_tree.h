@@ -26,7 +26,51 @@ constexpr int kTreeThreads = 64 * kTreeWaves;
 // Row tiles of 16 that a wave takes at most: its registers hold D / 4 values of the output and
 // D / 8 * terms of the queries for each (these go to the LDS where there are many).
 constexpr int tree_tiles_most(int terms, int d) { return terms == 1 ? (d > 128 ? 2 : 4) : (d > 128 ? 1 : 2); }
-constexpr bool tree_query_shared(int terms, int d, int tiles) { return terms * d * tiles > 256; }
+constexpr bool tree_query_shared(int terms, int d, int tiles) { return terms * d * tiles >= 256; }
+// Workgroups of a compute unit, and steps that a wave's loads are ahead of it.
+constexpr int tree_groups(int terms, int d, int tiles) { return 2; }
+constexpr int tree_ahead(int terms, int d, int tiles) { return d * tiles >= 512 ? 1 : d > 128 ? 1 : 2; }
+
+// Codes of a step of 32 tokens on their way from memory, in memory's order: piece x of 16 bytes of a tile
+// of 16 tokens is lane x % 64's, register x / 64. (Loaded as the products want them, a token's pieces
+// 16 lanes apart, each lane's piece was a look-up of the cache of its own: three times as many, which took
+// longer than the arithmetic.)
+template <int D>
+struct Raw {
+  u32x4 k[2][D / 64], v[2][D / 64];
+};
+
+// Where chunk c of 16 bytes of a token's codes lies in the LDS: moved within its rows so that the lanes
+// of a load, the same chunk of many tokens, take all banks.
+template <int D>
+__device__ __forceinline__ int code_place(int tok, int c) {
+  return tok * D + ((c ^ (D == 64 ? (tok >> 1) & 3 : tok & 7)) << 4);
+}
+
+// Eight codes of the LDS at `p`, transposed with those of the other lanes of a row of 16: lane 2 i
+// and 2 i + 1 name the first and the second eight of sixteen codes of token i, lane n gets code n of
+// the eight tokens.
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x2 transposed(const uint8_t* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                       (__attribute__((address_space(3))) i32x2*)p));
+}
+
+// Two codes (the low or the high half of a word) as a bf16 pair, times the power of two in the exponent
+// field of `pow`.
+template <bool HI>
+__device__ __forceinline__ uint32_t codes_times(uint32_t w, float pow) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, pow, HI));
+}
+
+// The greater of two values, NaN where one is (fmaxf would first make every operand canonical).
+__device__ __forceinline__ float greater(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+template <int BY>
+__device__ __forceinline__ float lane_greater(float x) {
+  float a, b;
+  lane_pair<BY>(x, a, b);
+  return greater(a, b);
+}
 
 struct TreeItem {
   int32_t r, tile;             // request, row tile
@@ -68,7 +112,10 @@ struct TreeShared {
   static constexpr bool kShared = tree_query_shared(TERMS, D, R);
   static constexpr int kTogether = D > 128 || R == 1 ? 1 : 2;  // row tiles joined at a time
   union {
-    bf16x8 q[kShared ? R * (D / 32) * TERMS * 64 : 1];         // [tile][chunk][term][lane]
+    struct {
+      bf16x8 q[kShared ? R * (D / 32) * TERMS * 64 : 1];       // [tile][chunk][term][lane]
+      uint8_t codes[kTreeWaves][kStep * D];                    // of K, then of V: each wave its own
+    };
     float acc[kTreeWaves][16 * kTogether][D + 4];              // the waves' results
   };
   float m[kTreeWaves][16 * R], l[kTreeWaves][16 * R];
@@ -76,40 +123,38 @@ struct TreeShared {
   float cost[kTreeWaves];
   int sums[kTreeWaves];
   int first;
-  int flag;
 };
 
-// Partial results of a range: quads of columns in two planes of pairs, row after row, so that a
-// wave's stores fill whole lines; then the exponent and the sum of each row.
+// Partial results of a range of a cut tile: quads of columns, row after row, then the exponent and the
+// sum of each row. The join is a launch of its own, so they are stored and loaded like any other data.
 template <int D, int R>
 struct TreePart {
-  static constexpr int64_t kFloats = (int64_t)16 * R * (D + 4);
+  static constexpr int64_t kFloats = (int64_t)16 * R * (D + 2);
   float* at;
-  __device__ __forceinline__ float* pair(int x, int plane) const {
-    return at + plane * (16 * R * D / 2) + 2 * x;
-  }
-  __device__ __forceinline__ void put_quad(int x, f32x4 v) const {
-    put_part(pair(x, 0), v[0], v[1]);
-    put_part(pair(x, 1), v[2], v[3]);
-  }
-  __device__ __forceinline__ f32x4 quad(int x) const {
-    float v[4];
-    get_part(pair(x, 0), v[0], v[1]);
-    get_part(pair(x, 1), v[2], v[3]);
-    return f32x4{v[0], v[1], v[2], v[3]};
-  }
-  __device__ __forceinline__ float* stat(int level, int row) const {
-    return at + 16 * R * (D + 2 * level) + 2 * row;
+  __device__ __forceinline__ f32x4* quad(int x) const { return reinterpret_cast<f32x4*>(at) + x; }
+  __device__ __forceinline__ f32x2v* stat(int row) const {
+    return reinterpret_cast<f32x2v*>(at + 16 * R * D) + row;
   }
 };
 template <int D, int R>
 __device__ __forceinline__ TreePart<D, R> tree_part(const TreeAttention& a, int h, int place) {
   return {a.a.few_part + ((int64_t)h * a.a.few_max + place) * TreePart<D, R>::kFloats};
 }
+// Where the partial results of a tile's range i are. A span has two places: for a range at its beginning,
+// and for one that begins in it and goes on behind it, as the first range of a tile may.
+__device__ __forceinline__ int tree_slot(int first, int mid, int i) {
+  return i == 0 ? 2 * first + mid : 2 * (first + i);
+}
+// What the join has to know of the range in a place.
+struct TreeCut {
+  int32_t splits;              // ranges of its tile; 0: nothing is there
+  int32_t part;                // its number among them
+  int32_t first, mid;          // the span of the first of them, and its place there
+  int32_t row0, rho0, live;    // the request's first row; the tile's first of its rows times the group, and how many
+};
 
-__device__ __forceinline__ RowPlace tree_place(const TreeAttention& a, const TreeItem& it, int h,
-                                               int rho) {
-  return {it.row0 + rho / a.a.G, h * a.a.G + rho % a.a.G};
+__device__ __forceinline__ RowPlace tree_place(const TreeAttention& a, int row0, int h, int rho) {
+  return {row0 + rho / a.a.G, h * a.a.G + rho % a.a.G};
 }
 
 // Bits lo .. hi - 1 of a word of 32 (any lo, hi).
@@ -150,9 +195,12 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
   constexpr int DW = D / 16;                     // columns of a lane
   constexpr int ES = TERMS == 1 ? 2 : 4;
   constexpr int PT = TERMS == 1 ? 2 : 3;         // terms of a weight
+  constexpr int kAhead = tree_ahead(TERMS, D, R);
   constexpr bool kShared = tree_query_shared(TERMS, D, R);
   const QAttention& a = ta.a;
-  const int lane = anew(threadIdx.x & 63), wave = threadIdx.x >> 6;
+  // (the wave's number in a scalar register: its steps are the same for all lanes then, and no wait
+  // for loads counts on a path on which some lanes skip a step)
+  const int lane = anew(threadIdx.x & 63), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int rho0 = it.tile * 16 * R;
 
@@ -186,7 +234,7 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
       for (int c = 0; c < D / 32; ++c) query(j, c, q[j][c]);
   }
 
-  f32x4 acc[R][DW];                              // acc[.][j][i]: column (4g + i) * D / 16 + j of row n
+  f32x4 acc[R][DW];                              // acc[.][c][i]: column 16 c + 4 g + i of row n
   float ref[R], l[R];                            // exponent that acc and l are relative to
 #pragma unroll
   for (int j = 0; j < R; ++j) {
@@ -200,12 +248,15 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
   const int B = 1 << a.b_shift;
   const int64_t page_codes = ((int64_t)a.H << a.b_shift) * D;
   const int64_t head_codes = ((int64_t)h << a.b_shift) * D;
-  const uint32_t k_lane = n * D + g * 16, v_lane = 4 * g * D + n * DW;
+  // a lane's pieces in the LDS: as they come from memory, and as the products want them
+  uint8_t* staged = lds.codes[wave];
+  constexpr int kPieces = D / 16;                // of a token
+  const uint32_t put = code_place<D>(lane / kPieces, lane % kPieces), lane_at = lane * 16;
   // 64 tiles of 16 tokens at a time: their pages and scales, one lane each
   for (int t0 = begin; t0 < end; t0 += 64 * 16) {
     int32_t my_page = 0;
     // (not 0, also where the softmax scale is: hidden scores are -inf times it)
-    float my_ks = 0x1p-126f, my_vs = 0.f;
+    float my_ks = 0x1p-126f, my_vs = 1.f;
     const int my_t = t0 + lane * 16;
     bool there = false;
     if (my_t < end) {
@@ -213,47 +264,58 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
       there = my_page >= 0 && my_page < a.pages;
       if (!there) my_page = 0;
       my_ks = fmaxf(a.ks[(int64_t)my_page * a.H + h] * a.scale_log2, 0x1p-126f);
-      my_vs = a.vs[(int64_t)my_page * a.H + h];
+      if (there) my_vs = a.vs[(int64_t)my_page * a.H + h];
     }
+    // V's scale as a power of two, which the conversion of its codes takes, times a rest in [1, 2),
+    // which the weights' exponent takes; their sum is divided by it. (An exponent field of 0 stands for
+    // 2^-127 in the conversion; a scale of 0 is that.)
+    const uint32_t vs_exponent = __float_as_uint(my_vs) & 0x7F800000u;
+    const float my_vp = __uint_as_float(vs_exponent);
+    const float rest = vs_exponent ? __uint_as_float((__float_as_uint(my_vs) & 0x7FFFFFu) | 0x3F800000u)
+                       : my_vs == 0.f ? 1.f : fabsf(my_vs) * 0x1p127f;
+    const float my_vl = __builtin_amdgcn_logf(rest), my_vi = 1.f / rest;
     const uint64_t absent = ~__ballot(there);
     const int steps = ((end < t0 + 1024 ? end : t0 + 1024) - t0 + kStep - 1) / kStep;
-    Loaded<D> x;
+    Raw<D> ring[kAhead];
     const auto base_of = [&](int tile) {
       const int64_t page = __builtin_amdgcn_readlane(my_page, tile);
       return page * page_codes + head_codes + (int64_t)((t0 + tile * 16) & (B - 1)) * D;
     };
-    const auto load_k = [&](int s) {
+    const auto load = [&](int s, const uint8_t* codes, u32x4 (&x)[2][D / 64]) {
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const uint8_t* kp = a.kc + base_of(2 * s + b);
+        const uint8_t* p = codes + base_of(2 * s + b);
 #pragma unroll
-        for (int c = 0; c < D / 64; ++c) x.k[b][c] = *global_ptr<u32x4>(kp + (k_lane + c * 64));
+        for (int c = 0; c < D / 64; ++c) x[b][c] = *global_ptr<u32x4>(p + (lane_at + c * 1024));
       }
     };
-    const auto load_v = [&](int s) {
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint8_t* vp = a.vc + base_of(2 * s + b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_columns<D>(x.v[b][i], vp + (v_lane + i * D));
-      }
-    };
-    load_k(0);
-    load_v(0);
-    // K of the next step is on its way from the scores on, V from the products on
-    for (int s = 0; s < steps; ++s) {
+    // K of the kAhead-th next step is on its way from the scores on, V from the products on
+    const auto step = [&](int s, Raw<D>& raw) {
       const int t = t0 + s * kStep;
+      const int next = s + kAhead < steps ? s + kAhead : steps - 1;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)         // (1024 bytes on: 1024 / D tokens, 4 where D is 256)
+          *reinterpret_cast<u32x4*>(staged + (D > 128 ? put ^ ((c & 1) << 6) : put) +
+                                    (b * 16 * D + c * 1024)) = raw.k[b][c];
+      load(next, a.kc, raw.k);
       f32x4 sc[R][2];
 #pragma unroll
       for (int j = 0; j < R; ++j) sc[j][0] = sc[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
       const int q_lane = kShared ? anew(lane) : lane;
+      const int kn = anew(n), kg = anew(g);
+      u32x4 chunk[2];
 #pragma unroll
       for (int c = 0; c < D / 64; ++c)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           bf16x8 k[2];
 #pragma unroll
-          for (int b = 0; b < 2; ++b) k[b] = operand(x.k[b][c][2 * half], x.k[b][c][2 * half + 1]);
+          for (int b = 0; b < 2; ++b) {
+            if (half == 0) chunk[b] = *reinterpret_cast<const u32x4*>(staged + code_place<D>(b * 16 + kn, 4 * c + kg));
+            k[b] = operand(chunk[b][2 * half], chunk[b][2 * half + 1]);
+          }
 #pragma unroll
           for (int j = 0; j < R; ++j)
 #pragma unroll
@@ -266,85 +328,94 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
                 sc[j][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b], qw, sc[j][b], 0, 0, 0);
             }
         }
-      if (s + 1 < steps) load_k(s + 1);
-      float kf[2], vs[2];
+      const auto of_tile = [&](float x, int b) {
+        return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 2 * s + b));
+      };
+      // V's codes follow K's in the same place
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        kf[b] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_ks), 2 * s + b));
-        vs[b] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(my_vs), 2 * s + b));
-      }
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c)
+          *reinterpret_cast<u32x4*>(staged + (D > 128 ? put ^ ((c & 1) << 6) : put) +
+                                    (b * 16 * D + c * 1024)) = raw.v[b][c];
+      load(next, a.vc, raw.v);
       // steps that some row sees only in part, or with absent pages
       const bool partly = t < all_lo || t + kStep > all_hi || ((absent >> (2 * s)) & 3) != 0;
-      uint32_t sees[R];                          // bit 4 b + i: the lane's tokens
-#pragma unroll
-      for (int j = 0; j < R; ++j) sees[j] = 0xFFu;
-      if (partly) {
+      uint32_t seen = 0;                         // bit 8 j + 4 b + i: the lane's tokens, row tile j
+      if (__builtin_expect(partly, 0)) {
         uint32_t there2 = (absent >> (2 * s)) & 1 ? 0u : 0xFFFFu;
         there2 |= (absent >> (2 * s + 1)) & 1 ? 0u : 0xFFFF0000u;
-        uint32_t odd = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-#pragma unroll
-          for (int w = 0; w < D / 64; ++w) odd |= nan_codes(x.v[k >> 2][k & 3][w]);
-        const bool any_odd = __any(odd != 0);
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-          const uint32_t y = tree_sees(ta, it, (rho0 + 16 * j + n) / a.G, t) & there2;
-          sees[j] = ((y >> (4 * g)) & 0xFu) | ((y >> (16 + 4 * g)) & 0xFu) << 4;
+          const int ln = lane_anew();            // (or what is made of it would be kept through the steps)
+          const uint32_t y = tree_sees(ta, it, (rho0 + 16 * j + (ln & 15)) / a.G, t) & there2;
+          const int lg = ln >> 4;
+          const uint32_t mine = ((y >> (4 * lg)) & 0xFu) | ((y >> (16 + 4 * lg)) & 0xFu) << 4;
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            sc[j][k >> 2][k & 3] = (sees[j] >> k) & 1 ? sc[j][k >> 2][k & 3] : kNone;
+            sc[j][k >> 2][k & 3] = (mine >> k) & 1 ? sc[j][k >> 2][k & 3] : kNone;
+          seen |= mine << (8 * j);
         }
-        // NaN codes of V are taken out of the product (0 * NaN would reach rows that do
-        // not see them); a product of their own finds the rows that do
-        if (any_odd) {
+        // NaN codes are taken out of the product (0 * NaN would reach rows that do not see them); a
+        // product of their own finds the rows that do
+        uint32_t odd = 0;
 #pragma unroll
-          for (int w = 0; w < D / 64; ++w) {
-            uint32_t bad[8];
+        for (int x = 0; x < D / 32; ++x) {
+          const u32x4 w = reinterpret_cast<const u32x4*>(staged)[64 * x + lane_anew()];
+          odd |= nan_codes(w[0]) | nan_codes(w[1]) | nan_codes(w[2]) | nan_codes(w[3]);
+        }
+        if (__any(odd != 0)) {
+          const int ln = lane_anew(), lc = ln & 15;
+          const uint32_t token = 4 * (ln >> 4) + ((lc >> 1) & 3) + 16 * (lc >> 3);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) bad[k] = nan_codes((uint32_t)anew((int)x.v[k >> 2][k & 3][w]));
+          for (int c = 0; c < DW; ++c) {
+            const u32x2 w = transposed(staged + code_place<D>(token, c) + 8 * (lc & 1));
+            u32x4 is;                            // 1 where the code is NaN
 #pragma unroll
-            for (int o = 0; o < 4; ++o) {
-              u32x4 is;                          // 1 where the code is NaN
-#pragma unroll
-              for (int k = 0; k < 4; ++k)
-                is[k] = ((bad[2 * k] >> (8 * o)) & 1) * 0x3F80u |
-                        ((bad[2 * k + 1] >> (8 * o)) & 1) * 0x3F800000u;
-#pragma unroll
-              for (int j = 0; j < R; ++j) {
-                u32x4 by;                        // 1 where the lane's row sees the token
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  by[k] = ((sees[j] >> (2 * k)) & 1 ? 0x3F80u : 0u) |
-                          ((sees[j] >> (2 * k + 1)) & 1 ? 0x3F800000u : 0u);
-                f32x4 hits = {0.f, 0.f, 0.f, 0.f};
-                hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is),
-                                                               __builtin_bit_cast(bf16x8, by), hits, 0,
-                                                               0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  if (hits[i] > 0.f) acc[j][4 * w + o][i] = __builtin_nanf("");
-              }
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t y = nan_codes(w[k >> 1]) >> (16 * (k & 1));
+              is[k] = (y & 1) * 0x3F80u | ((y >> 8) & 1) * 0x3F800000u;
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) x.v[k >> 2][k & 3][w] &= ~(bad[k] * 0xFFu);
+            for (int j = 0; j < R; ++j) {
+              u32x4 by;                          // 1 where the lane's row sees the token
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                by[k] = ((seen >> (8 * j + 2 * k)) & 1) * 0x3F80u |
+                        ((seen >> (8 * j + 2 * k + 1)) & 1) * 0x3F800000u;
+              f32x4 hits = {0.f, 0.f, 0.f, 0.f};
+              hits = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, is),
+                                                             __builtin_bit_cast(bf16x8, by), hits, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (hits[i] > 0.f) acc[j][c][i] = __builtin_nanf("");
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x) {
+            u32x4* at = reinterpret_cast<u32x4*>(staged) + (64 * x + lane_anew());
+            u32x4 w = *at;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] &= ~(nan_codes(w[k]) * 0xFFu);
+            *at = w;
           }
         }
       }
       bf16x8 pt[R][PT];
 #pragma unroll
       for (int j = 0; j < R; ++j) {
-        float best = kNone;
+        float best[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          float y = sc[j][b][0];
+          best[b] = sc[j][b][0];
 #pragma unroll
-          for (int i = 1; i < 4; ++i) y = fmaxf(y, sc[j][b][i]);
-          best = fmaxf(best, y * kf[b]);
+          for (int i = 1; i < 4; ++i) best[b] = greater(best[b], sc[j][b][i]);
         }
-        best = lane_max<32>(lane_max<16>(best));
-        if (__any(best > ref[j] + 8.f)) {
-          const float m = fmaxf(ref[j], best);
+        float top = greater(best[0] * of_tile(my_ks, 0), best[1] * of_tile(my_ks, 1));
+        top = lane_greater<32>(lane_greater<16>(top));
+        // (a NaN among them: the row is NaN in any case)
+        if (__any(top > ref[j] + 8.f)) {
+          const float m = fmaxf(ref[j], top);
           const float shrink = m == kNone ? 1.f : __builtin_amdgcn_exp2f(ref[j] - m);
           l[j] *= shrink;
 #pragma unroll
@@ -356,42 +427,56 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
         const float low = ref[j] == kNone ? 0.f : ref[j];
         float pv[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float pr = __builtin_amdgcn_exp2f(fmaf(sc[j][k >> 2][k & 3], kf[k >> 2], -low));
-          l[j] += pr;
-          pv[k] = pr * vs[k >> 2];
-        }
-        if (partly) {                            // (a scale may be NaN where nothing is seen)
+        for (int b = 0; b < 2; ++b) {
+          const float off = of_tile(my_vl, b) - low, kf = of_tile(my_ks, b);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) pv[k] = (sees[j] >> k) & 1 ? pv[k] : 0.f;
+          for (int i = 0; i < 4; ++i)
+            pv[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(sc[j][b][i], kf, off));
+          l[j] = fmaf((pv[4 * b] + pv[4 * b + 1]) + (pv[4 * b + 2] + pv[4 * b + 3]), of_tile(my_vi, b), l[j]);
         }
         split_terms<PT>(pv, pt[j]);
       }
+      // out^T += V^T P^T, 16 columns at a time: lane n of the operand is column n, its eight tokens
+      // 4 g .. 4 g + 3 of both tiles
+      const uint32_t token = 4 * kg + ((kn >> 1) & 3) + 16 * (kn >> 3);
 #pragma unroll
-      for (int w = 0; w < D / 64; ++w) {
+      for (int c = 0; c < DW; ++c) {
+        const u32x2 w = transposed(staged + code_place<D>(token, c) + 8 * (kn & 1));
+        u32x4 vt;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t c[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            c[k] = half ? codes_bf16<true>(x.v[k >> 2][k & 3][w]) : codes_bf16<false>(x.v[k >> 2][k & 3][w]);
-#pragma unroll
-          for (int o = 0; o < 2; ++o) {
-            u32x4 vt;
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              vt[k] = __builtin_amdgcn_perm(c[2 * k + 1], c[2 * k], o ? 0x07060302u : 0x05040100u);
-            const int col = 4 * w + 2 * half + o;
-#pragma unroll
-            for (int z = PT - 1; z >= 0; --z)
-#pragma unroll
-              for (int j = 0; j < R; ++j)
-                acc[j][col] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt),
-                                                                      pt[j][z], acc[j][col], 0, 0, 0);
-          }
+        for (int b = 0; b < 2; ++b) {
+          const float pow = of_tile(my_vp, b);
+          vt[2 * b] = codes_times<false>(w[b], pow);
+          vt[2 * b + 1] = codes_times<true>(w[b], pow);
         }
+#pragma unroll
+        for (int z = PT - 1; z >= 0; --z)
+#pragma unroll
+          for (int j = 0; j < R; ++j)
+            acc[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), pt[j][z],
+                                                                acc[j][c], 0, 0, 0);
       }
-      if (s + 1 < steps) load_v(s + 1);
+    };
+#pragma unroll
+    for (int y = 0; y < kAhead; ++y)
+    {
+      // (in the order of the steps: a wait for the first of them is then not one for all)
+      load(y < steps ? y : steps - 1, a.kc, ring[y].k);
+      __builtin_amdgcn_sched_barrier(0);
+      load(y < steps ? y : steps - 1, a.vc, ring[y].v);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // (out of the loop at once where they end: a path around a step would have every wait for
+    // loads count on those that it did not issue)
+    for (int s = 0;;) {
+      bool over = false;
+#pragma unroll
+      for (int y = 0; y < kAhead; ++y) {
+        if (over) break;
+        step(s, ring[y]);
+        over = ++s >= steps;
+      }
+      if (over) break;
     }
   }
 
@@ -413,14 +498,9 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
     __syncthreads();                             // (also: the queries in the LDS are not needed now)
 #pragma unroll
     for (int jj = 0; jj < kTogether; ++jj) {
-      float* row = &lds.acc[wave][16 * jj + en][4 * eg * DW];
+      float* row = &lds.acc[wave][16 * jj + en][4 * eg];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int c = 0; c < DW; c += 4)
-          *reinterpret_cast<f32x4*>(&row[i * DW + c]) =
-              f32x4{acc[j0 + jj][c][i], acc[j0 + jj][c + 1][i], acc[j0 + jj][c + 2][i],
-                    acc[j0 + jj][c + 3][i]};
+      for (int c = 0; c < DW; ++c) *reinterpret_cast<f32x4*>(&row[16 * c]) = acc[j0 + jj][c];
     }
     __syncthreads();
     constexpr int kQuads = D / 4;
@@ -442,75 +522,21 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
         for (int i = 0; i < 4; ++i) o[i] += f * v[i];
       }
       if (it.splits == 1) {
-        const RowPlace place = tree_place(ta, it, h, rho0 + row);
+        const RowPlace place = tree_place(ta, it.row0, h, rho0 + row);
         put_quad<ES>(a, place, 4 * quad, o, sum);
         if (quad == 0) put_lse(a, place, low, sum);
       } else {
-        part.put_quad(row * kQuads + quad, o);
-        if (quad == 0) put_part(part.stat(0, row), m, sum);
+        *part.quad(row * kQuads + quad) = o;
+        if (quad == 0) *part.stat(row) = f32x2v{m, sum};
       }
     }
   }
   __syncthreads();                               // (the LDS is the next range's)
 }
 
-// Joins `count` partial results of a tile, in the places slot(0), slot(1), ..: into the output (`whole`)
-// or, as the result of a group, into the first of them.
-template <int D, int R, int ES, class Slot>
-__device__ __forceinline__ void tree_join(const TreeAttention& ta, const TreeItem& it, int h, int count,
-                                          int level, bool whole, Slot slot) {
-  constexpr int kQuads = D / 4, kBatch = 8;
-  const int rho0 = it.tile * 16 * R;
-  const int live = it.count * ta.a.G - rho0;
-  const int total = (live < 16 * R ? live : 16 * R) * kQuads;
-  const TreePart<D, R> p0 = tree_part<D, R>(ta, h, slot(0));
-  for (int x = anew(threadIdx.x); x < total; x += kTreeThreads) {
-    const int row = x / kQuads;
-    Joined sum;
-    for (int s = 0; s < count; s += kBatch) {
-      f32x4 o[kBatch];
-      float m[kBatch], l[kBatch];
-#pragma unroll
-      for (int k = 0; k < kBatch; ++k) {
-        const TreePart<D, R> p = tree_part<D, R>(ta, h, slot(s + k < count ? s + k : s));
-        o[k] = p.quad(x);
-        get_part(p.stat(level, row), m[k], l[k]);
-      }
-      sum.add(o, m, l, count - s);
-    }
-    if (whole) {
-      const RowPlace place = tree_place(ta, it, h, rho0 + row);
-      put_quad<ES>(ta.a, place, 4 * (x % kQuads), sum.o, sum.l);
-      if (x % kQuads == 0) put_lse(ta.a, place, sum.m == kNone ? 0.f : sum.m, sum.l);
-    } else {
-      p0.put_quad(x, sum.o);                     // (read by this thread alone)
-      if (x % kQuads == 0) put_part(p0.stat(1, row), sum.m, sum.l);
-    }
-  }
-}
-
-// After one of a tile's partial results, number `split`, is written: the last workgroup of every
-// kJoin of them (more where there are more than kJoin^2) joins these, the last of the groups joins the
-// groups. Which workgroup comes last changes nothing.
-template <int D, int R, int ES, class Slot>
-__device__ __forceinline__ void tree_finish(const TreeAttention& ta, const TreeItem& it, int h, int split,
-                                            int* s_flag, Slot slot) {
-  int32_t* counters = ta.a.few_count + 2 * (int64_t)h * ta.a.few_max;
-  const int splits = it.splits;
-  int size = kJoin;
-  while (size * size < splits) size += kJoin;
-  const int group = split / size, groups = (splits + size - 1) / size;
-  const int here = group * size, members = splits - here < size ? splits - here : size;
-  if (!last_to_come(counters + 2 * slot(here), members, s_flag)) return;
-  tree_join<D, R, ES>(ta, it, h, members, 0, groups == 1, [&](int i) { return slot(here + i); });
-  if (groups == 1) return;
-  if (!last_to_come(counters + 2 * slot(0) + 1, groups, s_flag)) return;
-  tree_join<D, R, ES>(ta, it, h, groups, 1, true, [&](int i) { return slot(i * size); });
-}
-
 // The ranges of a workgroup's span, one after another.
 template <int TERMS, int D, int R>
-__global__ __launch_bounds__(kTreeThreads, 2) void qcache_tree_kernel(TreeAttention ta) {
+__global__ __launch_bounds__(kTreeThreads, tree_groups(TERMS, D, R)) void qcache_tree_kernel(TreeAttention ta) {
   __shared__ TreeShared<TERMS, D, R> lds;
   constexpr int ES = TERMS == 1 ? 2 : 4;
   constexpr int kPer = CM_QCACHE_MAX_REQUESTS / kTreeThreads;
@@ -519,6 +545,10 @@ __global__ __launch_bounds__(kTreeThreads, 2) void qcache_tree_kernel(TreeAttent
   const HeadItem hi = head_item(a.H, blockIdx.x);
   const int h = hi.h, w = hi.item;
   if (w >= a.few_items) return;
+  // (the heads' spans are the same)
+  TreeCut* cuts = static_cast<TreeCut*>(a.many_found) + 2 * w;
+  const bool tells = h == 0 && threadIdx.x == 0;
+  if (tells) cuts[0].splits = cuts[1].splits = 0;
 
   // where every request begins: prefix sums of the units of all its tiles
   const int per = (a.n + kTreeThreads - 1) / kTreeThreads;
@@ -595,41 +625,113 @@ __global__ __launch_bounds__(kTreeThreads, 2) void qcache_tree_kernel(TreeAttent
     it.end = end < it.len ? (int)end : it.len;
     const int first = tile_from / span, part = w - first;
     it.splits = (tile_to - 1) / span - first + 1;
-    // (in the first of them another range may come before it)
-    const auto slot = [&](int i) {
-      return i == 0 ? 2 * first + (tile_from > first * span ? 1 : 0) : 2 * (first + i);
-    };
-    tree_segment<TERMS, D, R>(ta, it, h, slot(part), lds);
-    if (it.splits > 1) tree_finish<D, R, ES>(ta, it, h, part, &lds.flag, slot);
+    const int mid = part == 0 && tile_from > first * span ? 1 : 0;
+    if (it.splits > 1 && tells) {
+      const int rho0 = it.tile * 16 * R, live = it.count * a.G - rho0;
+      cuts[mid] = TreeCut{it.splits, part, first, tile_from > first * span ? 1 : 0, it.row0, rho0,
+                          live < 16 * R ? live : 16 * R};
+    }
+    tree_segment<TERMS, D, R>(ta, it, h, 2 * w + mid, lds);
     if (u == to) ++r;
   }
 }
 
+// Joins the partial results of the tiles that are cut: the workgroup of each range takes an equal part of
+// its tile's quads of columns, over the results of all its ranges; threads that share a quad take every
+// kth result, in an order that depends on their number alone. (Joined by the last workgroups of the launch
+// before to come, with stores and loads past the caches of the XCDs, 64 rows over 264 thousand tokens
+// took 50 us longer than their arithmetic; so 12.)
+constexpr int kTreeJoin = 256;
+template <int D, int R, int ES>
+__global__ __launch_bounds__(kTreeJoin) void qcache_tree_join_kernel(TreeAttention ta) {
+  constexpr int kQuads = D / 4, kBatch = 8;
+  __shared__ f32x4 s_o[kTreeJoin];
+  __shared__ float s_m[kTreeJoin], s_l[kTreeJoin];
+  const QAttention& a = ta.a;
+  const HeadItem hi = head_item(a.H, blockIdx.x);
+  const int h = hi.h, w = hi.item, tid = threadIdx.x;
+  if (w >= a.few_items) return;
+  for (int mid = 0; mid < 2; ++mid) {
+    const TreeCut cut = static_cast<const TreeCut*>(a.many_found)[2 * w + mid];
+    if (cut.splits == 0) continue;
+    const int total = cut.live * kQuads, share = (total + cut.splits - 1) / cut.splits;
+    const int begin = cut.part * share, end = begin + share < total ? begin + share : total;
+    // the quads of a pass, a power of two, and the threads that share one
+    int width = 1;
+    while (width < end - begin && width < kTreeJoin) width *= 2;
+    const int sharers = kTreeJoin / width, q = tid & (width - 1), p = tid / width;
+    for (int x0 = begin; x0 < end; x0 += width) {
+      const int x = x0 + q < end ? x0 + q : end - 1, row = x / kQuads;
+      Joined sum;
+      for (int s = p; s < cut.splits; s += sharers * kBatch) {
+        f32x4 o[kBatch];
+        float m[kBatch], l[kBatch];
+        int there = 0;
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          const int i = s + k * sharers < cut.splits ? s + k * sharers : s;
+          there += s + k * sharers < cut.splits;
+          const TreePart<D, R> part = tree_part<D, R>(ta, h, tree_slot(cut.first, cut.mid, i));
+          o[k] = *part.quad(x);
+          const f32x2v st = *part.stat(row);
+          m[k] = st[0];
+          l[k] = st[1];
+        }
+        sum.add(o, m, l, there);
+      }
+      if (sharers > 1) {
+        s_o[tid] = sum.o;
+        s_m[tid] = sum.m;
+        s_l[tid] = sum.l;
+        __syncthreads();
+        for (int half = sharers / 2; half > 0; half >>= 1) {
+          if (p < half) {
+            f32x4 o[1] = {s_o[tid + half * width]};
+            float m[1] = {s_m[tid + half * width]}, l[1] = {s_l[tid + half * width]};
+            sum.add(o, m, l, 1);
+            s_o[tid] = sum.o;
+            s_m[tid] = sum.m;
+            s_l[tid] = sum.l;
+          }
+          __syncthreads();
+        }
+      }
+      if (p == 0 && x0 + q < end) {
+        const RowPlace place = tree_place(ta, cut.row0, h, cut.rho0 + row);
+        put_quad<ES>(a, place, 4 * (x % kQuads), sum.o, sum.l);
+        if (x % kQuads == 0) put_lse(a, place, sum.m == kNone ? 0.f : sum.m, sum.l);
+      }
+    }
+  }
+}
+
+template <int TERMS, int D, int R>
+hipError_t launch_tree_tiles(const TreeAttention& a, hipStream_t stream) {
+  const dim3 groups((uint32_t)head_groups(a.a.H, a.a.few_items));
+  hipLaunchKernelGGL((qcache_tree_kernel<TERMS, D, R>), groups, dim3(kTreeThreads), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.a.few_items == 1) return e;  // (one span for each head: nothing is cut)
+  hipLaunchKernelGGL((qcache_tree_join_kernel<D, R, TERMS == 1 ? 2 : 4>), groups, dim3(kTreeJoin), 0, stream, a);
+  return hipGetLastError();
+}
 template <int TERMS>
-hipError_t launch_tree(const TreeAttention& a, int32_t d, int32_t tiles, uint32_t groups,
-                       hipStream_t stream) {
-  const auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3(groups), dim3(kTreeThreads), 0, stream, a);
-    return hipGetLastError();
-  };
+hipError_t launch_tree(const TreeAttention& a, int32_t d, int32_t tiles, hipStream_t stream) {
   if (d == 64) {
     if constexpr (TERMS == 1)
-      if (tiles == 4) return go(qcache_tree_kernel<TERMS, 64, 4>);
-    return tiles == 1 ? go(qcache_tree_kernel<TERMS, 64, 1>) : go(qcache_tree_kernel<TERMS, 64, 2>);
+      if (tiles == 4) return launch_tree_tiles<TERMS, 64, 4>(a, stream);
+    return tiles == 1 ? launch_tree_tiles<TERMS, 64, 1>(a, stream) : launch_tree_tiles<TERMS, 64, 2>(a, stream);
   }
   if (d == 128) {
     if constexpr (TERMS == 1)
-      if (tiles == 4) return go(qcache_tree_kernel<TERMS, 128, 4>);
-    return tiles == 1 ? go(qcache_tree_kernel<TERMS, 128, 1>) : go(qcache_tree_kernel<TERMS, 128, 2>);
+      if (tiles == 4) return launch_tree_tiles<TERMS, 128, 4>(a, stream);
+    return tiles == 1 ? launch_tree_tiles<TERMS, 128, 1>(a, stream) : launch_tree_tiles<TERMS, 128, 2>(a, stream);
   }
   if constexpr (TERMS == 1)
-    if (tiles == 2) return go(qcache_tree_kernel<TERMS, 256, 2>);
-  return go(qcache_tree_kernel<TERMS, 256, 1>);
+    if (tiles == 2) return launch_tree_tiles<TERMS, 256, 2>(a, stream);
+  return launch_tree_tiles<TERMS, 256, 1>(a, stream);
 }
 // (a file for each type of the queries: they are built side by side)
-hipError_t launch_tree_bf16(const TreeAttention& a, int32_t d, int32_t tiles, uint32_t groups,
-                            hipStream_t stream);
-hipError_t launch_tree_fp32(const TreeAttention& a, int32_t d, int32_t tiles, uint32_t groups,
-                            hipStream_t stream);
+hipError_t launch_tree_bf16(const TreeAttention& a, int32_t d, int32_t tiles, hipStream_t stream);
+hipError_t launch_tree_fp32(const TreeAttention& a, int32_t d, int32_t tiles, hipStream_t stream);
 
 }  // namespace cm

@@ -82,8 +82,8 @@ TreePlan plan_qcache_tree(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_
   const int64_t rows = (int64_t)(max_rows < n_rows ? max_rows : n_rows) * G;
   p.tiles = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
   p.tiles = p.tiles < most ? p.tiles : most;
-  // workgroups that run together: two on a compute unit
-  const int64_t groups = 2 * device_cu_count();
+  // workgroups that run together
+  const int64_t groups = (int64_t)tree_groups(terms, d, p.tiles) * device_cu_count();
   p.items = (int32_t)(groups / H > 0 ? groups / H : 1);
   p.places = 2 * p.items;                        // a span's first and last range
   // all contexts together, a request's once for each of its tiles, are less than 2e9 units
@@ -91,22 +91,21 @@ TreePlan plan_qcache_tree(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_
   p.unit = kTreeWaves * kStep;
   while (tiles * (double)(longest / p.unit + 1) > 1.9e9) p.unit *= 2;
   p.least = 2;
-  p.part_at = sizeof(int32_t) * kCounters;
-  p.bytes = p.part_at + sizeof(float) * (size_t)(16 * p.tiles) * (size_t)(d + 4) * (size_t)H * (size_t)p.places;
+  p.cuts_at = sizeof(int32_t) * kCounters;       // (counters are the causal attention's)
+  p.part_at = p.cuts_at + align_up(sizeof(TreeCut) * (size_t)p.places, kWsAlign);
+  p.bytes = p.part_at + sizeof(float) * (size_t)(16 * p.tiles) * (size_t)(d + 2) * (size_t)H * (size_t)p.places;
   return p;
 }
 
-hipError_t launch_tree_bf16(const TreeAttention& a, int32_t d, int32_t tiles, uint32_t groups,
-                            hipStream_t stream) {
-  return launch_tree<1>(a, d, tiles, groups, stream);
+hipError_t launch_tree_bf16(const TreeAttention& a, int32_t d, int32_t tiles, hipStream_t stream) {
+  return launch_tree<1>(a, d, tiles, stream);
 }
 
 hipError_t launch_qcache_tree_attention(const TreeAttention& a, int32_t d, int32_t dtype, int32_t tiles,
                                         hipStream_t stream) {
   ScopedTiming tm(K_QCACHE_TREE_ATTENTION, stream);
-  const uint32_t groups = (uint32_t)head_groups(a.a.H, a.a.few_items);
-  return dtype == CM_BF16 ? launch_tree_bf16(a, d, tiles, groups, stream)
-                          : launch_tree_fp32(a, d, tiles, groups, stream);
+  return dtype == CM_BF16 ? launch_tree_bf16(a, d, tiles, stream)
+                          : launch_tree_fp32(a, d, tiles, stream);
 }
 
 }  // namespace cm

@@ -3,9 +3,8 @@
 
 namespace cm {
 
-hipError_t launch_tree_fp32(const TreeAttention& a, int32_t d, int32_t tiles, uint32_t groups,
-                            hipStream_t stream) {
-  return launch_tree<3>(a, d, tiles, groups, stream);
+hipError_t launch_tree_fp32(const TreeAttention& a, int32_t d, int32_t tiles, hipStream_t stream) {
+  return launch_tree<3>(a, d, tiles, stream);
 }
 
 }  // namespace cm
