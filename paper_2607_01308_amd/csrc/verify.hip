@@ -25,6 +25,7 @@ constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
 constexpr int kVec = 8;              // elements of a lane's load
 constexpr int kStep = 64 * kVec;     // and of a wave's
+constexpr int kBatch = 3;            // steps whose loads are under way together
 
 // What is not a probability counts as none.
 __device__ __forceinline__ double clean(float x) {
@@ -37,32 +38,56 @@ __device__ __forceinline__ float element(const void* row, int64_t v) {
   else return __uint_as_float((uint32_t) * (global_ptr<uint16_t>(row) + v) << 16);
 }
 
-// kVec elements from v on; what lies behind V is 0. Rows begin at any element.
+// kVec elements from v on as they are in memory; rows begin at any element.
 typedef uint32_t words_f32 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t words_bf16 __attribute__((ext_vector_type(4), aligned(2)));
 template <int ES>
+struct Raw {
+  u32x4 w[ES / 2];
+};
+template <int ES>
+__device__ __forceinline__ Raw<ES> load_raw(const void* row, int64_t v) {
+  Raw<ES> x;
+  if constexpr (ES == 4) {
+    const CM_GLOBAL float* at = global_ptr<float>(row) + v;
+    x.w[0] = *(const CM_GLOBAL words_f32*)at;
+    x.w[1] = *(const CM_GLOBAL words_f32*)(at + 4);
+  } else {
+    x.w[0] = *(const CM_GLOBAL words_bf16*)(global_ptr<uint16_t>(row) + v);
+  }
+  return x;
+}
+template <int ES>
+__device__ __forceinline__ void unpack(const Raw<ES>& raw, float (&x)[kVec]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if constexpr (ES == 4) {
+      x[k] = __uint_as_float(raw.w[0][k]);
+      x[4 + k] = __uint_as_float(raw.w[1][k]);
+    } else {
+      x[2 * k] = low_bf16(raw.w[0][k]);
+      x[2 * k + 1] = high_bf16(raw.w[0][k]);
+    }
+  }
+}
+// The same as fp32; what lies behind V is 0.
+template <int ES>
 __device__ __forceinline__ void load(const void* row, int64_t v, int64_t V, float (&x)[kVec]) {
   if (v + kVec <= V) {
-    if constexpr (ES == 4) {
-      const CM_GLOBAL float* at = global_ptr<float>(row) + v;
-      const words_f32 a = *(const CM_GLOBAL words_f32*)at, b = *(const CM_GLOBAL words_f32*)(at + 4);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[k] = __uint_as_float(a[k]);
-        x[4 + k] = __uint_as_float(b[k]);
-      }
-    } else {
-      const words_bf16 a = *(const CM_GLOBAL words_bf16*)(global_ptr<uint16_t>(row) + v);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        x[2 * k] = low_bf16(a[k]);
-        x[2 * k + 1] = high_bf16(a[k]);
-      }
-    }
+    unpack<ES>(load_raw<ES>(row, v), x);
   } else {
 #pragma unroll
     for (int k = 0; k < kVec; ++k) x[k] = v + k < V ? element<ES>(row, v + k) : 0.f;
   }
+}
+// The greatest of the values' bits: 0x7F800000 or more where one is no probability (or -0).
+__device__ __forceinline__ uint32_t greatest_bits(uint32_t top, const float (&x)[kVec]) {
+#pragma unroll
+  for (int k = 0; k < kVec; ++k) {
+    const uint32_t y = __float_as_uint(x[k]);
+    top = top > y ? top : y;
+  }
+  return top;
 }
 
 struct VerifyShared {
@@ -70,6 +95,9 @@ struct VerifyShared {
   double sub[kWaves];                  // and of their steps
   int64_t hit[kWaves], any[kWaves];
   int64_t gone[CM_DRAFT_MAX_NODES];    // tokens taken out of r
+  int64_t drafts[CM_DRAFT_MAX_NODES];  // the request's nodes
+  int32_t parents[CM_DRAFT_MAX_NODES];
+  float accept[CM_DRAFT_MAX_NODES];
   int32_t n_gone;
 };
 
@@ -90,9 +118,16 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
       for (int64_t i = first + threadIdx.x; i < next; i += kThreads) a.path[i] = -1;
     return;
   }
-  const int32_t* parents = a.parents + first;
-  const int64_t* drafts = a.drafts + first;
-  const float* accept = a.accept + first;
+  for (int i = threadIdx.x; i < c; i += kThreads) {
+    lds.drafts[i] = a.drafts[first + i];
+    lds.parents[i] = a.parents[first + i];
+    lds.accept[i] = a.accept[first + i];
+  }
+  if (threadIdx.x == 0) lds.n_gone = 0;
+  __syncthreads();
+  const int32_t* parents = lds.parents;
+  const int64_t* drafts = lds.drafts;
+  const float* accept = lds.accept;
   int32_t* path = a.path + first;
 
   // The next child of node `of` after node `after`, c where there is none. (All waves look.)
@@ -120,18 +155,23 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
   // A wave's part of the row: whole steps.
   const int64_t part = ((V + kWaves - 1) / kWaves + kStep - 1) / kStep * kStep;
 
-  // r of the kVec elements from v on
-  const auto rest = [&](int64_t v, double M, double (&r)[kVec]) {
-    float x[kVec];
-    load<ES>(p, v, V, x);
-    if (sampled) {
-      float y[kVec];
-      load<ES>(q, v, V, y);
+  // r of kVec elements, from v on, with the probabilities x and y
+  const auto rest_of = [&](float (&x)[kVec], float (&y)[kVec], int64_t v, double M, double (&r)[kVec]) {
+    uint32_t top = greatest_bits(0, x);
+    if (sampled) top = greatest_bits(top, y);
+    if (__builtin_expect(__any(top >= 0x7F800000u), 0)) {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) r[k] = fmax(fma(-M, clean(y[k]), clean(x[k])), 0.0);
+      for (int k = 0; k < kVec; ++k) {
+        x[k] = (float)clean(x[k]);
+        if (sampled) y[k] = (float)clean(y[k]);
+      }
+    }
+    if (sampled) {
+#pragma unroll
+      for (int k = 0; k < kVec; ++k) r[k] = fmax(fma(-M, (double)y[k], (double)x[k]), 0.0);
     } else {
 #pragma unroll
-      for (int k = 0; k < kVec; ++k) r[k] = clean(x[k]);
+      for (int k = 0; k < kVec; ++k) r[k] = x[k];
       const int gone = lds.n_gone;
       for (int i = 0; i < gone; ++i) {
         const int64_t t = lds.gone[i] - v;
@@ -139,6 +179,12 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
         for (int k = 0; k < kVec; ++k) r[k] = t == k ? 0.0 : r[k];
       }
     }
+  };
+  const auto rest = [&](int64_t v, double M, double (&r)[kVec]) {
+    float x[kVec], y[kVec];
+    load<ES>(p, v, V, x);
+    if (sampled) load<ES>(q, v, V, y);
+    rest_of(x, y, v, M, r);
   };
   const auto sum_of = [](const double (&r)[kVec]) {
     double s = 0.0;
@@ -155,7 +201,25 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
   const auto total = [&](double M) {
     double s = 0.0;
     const int64_t begin = wave * part, end = begin + part < V ? begin + part : V;
-    for (int64_t v = begin + lane * kVec; v < end; v += kStep) {
+    int64_t v0 = begin;
+    for (; v0 + kBatch * kStep <= end; v0 += kBatch * kStep) {
+      Raw<ES> x[kBatch], y[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        x[b] = load_raw<ES>(p, v0 + b * kStep + lane * kVec);
+        if (sampled) y[b] = load_raw<ES>(q, v0 + b * kStep + lane * kVec);
+      }
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        float xs[kVec], ys[kVec];
+        double r[kVec];
+        unpack<ES>(x[b], xs);
+        if (sampled) unpack<ES>(y[b], ys);
+        rest_of(xs, ys, v0 + b * kStep + lane * kVec, M, r);
+        s += sum_of(r);
+      }
+    }
+    for (int64_t v = v0 + lane * kVec; v < end; v += kStep) {
       double r[kVec];
       rest(v, M, r);
       s += sum_of(r);
@@ -171,7 +235,6 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
   };
 
   double M = 0.0, m = 1.0;
-  if (threadIdx.x == 0) lds.n_gone = 0;
   while (true) {
     if (threadIdx.x == 0) path[count] = node;
     ++count;
