@@ -72,6 +72,27 @@ __device__ __forceinline__ float lane_greater(float x) {
   return greater(a, b);
 }
 
+// split_terms<2>, the rests x - x0 as dot products (exact: one factor is 1, the other 0), so that the
+// first terms are not taken apart again.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split_two(const float (&x)[8], bf16x8 (&out)[2]) {
+  // ((-1, 0) and (0, -1), out of the compiler's sight: the first as a constant of the instruction is
+  // taken for an fp32 -1, which is the second)
+  uint32_t one = 0x0000BF80u, two = 0xBF800000u;
+  asm("" : "+s"(one), "+s"(two));
+  const bf16x2 first = __builtin_bit_cast(bf16x2, one), second = __builtin_bit_cast(bf16x2, two);
+  u32x4 hi, lo;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    hi[k] = pair_bf16(x[2 * k], x[2 * k + 1]);
+    const bf16x2 both = __builtin_bit_cast(bf16x2, (uint32_t)hi[k]);
+    lo[k] = pair_bf16(__builtin_amdgcn_fdot2_f32_bf16(both, first, x[2 * k], false),
+                      __builtin_amdgcn_fdot2_f32_bf16(both, second, x[2 * k + 1], false));
+  }
+  out[0] = __builtin_bit_cast(bf16x8, hi);
+  out[1] = __builtin_bit_cast(bf16x8, lo);
+}
+
 struct TreeItem {
   int32_t r, tile;             // request, row tile
   int32_t row0, count, nodes;  // first row, rows that are computed, all of them
@@ -306,6 +327,7 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
       const int q_lane = kShared ? anew(lane) : lane;
       const int kn = anew(n), kg = anew(g);
       u32x4 chunk[2];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int c = 0; c < D / 64; ++c)
 #pragma unroll
@@ -328,6 +350,7 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
                 sc[j][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[b], qw, sc[j][b], 0, 0, 0);
             }
         }
+      __builtin_amdgcn_s_setprio(0);
       const auto of_tile = [&](float x, int b) {
         return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 2 * s + b));
       };
@@ -401,7 +424,9 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
           }
         }
       }
-      bf16x8 pt[R][PT];
+      // (each lane looks at its own tokens: that one of them has a new maximum is rare)
+      float top[R];
+      bool more = false;
 #pragma unroll
       for (int j = 0; j < R; ++j) {
         float best[2];
@@ -411,11 +436,15 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
 #pragma unroll
           for (int i = 1; i < 4; ++i) best[b] = greater(best[b], sc[j][b][i]);
         }
-        float top = greater(best[0] * of_tile(my_ks, 0), best[1] * of_tile(my_ks, 1));
-        top = lane_greater<32>(lane_greater<16>(top));
-        // (a NaN among them: the row is NaN in any case)
-        if (__any(top > ref[j] + 8.f)) {
-          const float m = fmaxf(ref[j], top);
+        top[j] = greater(best[0] * of_tile(my_ks, 0), best[1] * of_tile(my_ks, 1));
+        more |= top[j] > ref[j] + 8.f;
+      }
+      if (__any(more)) {
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          if (!__any(top[j] > ref[j] + 8.f)) continue;
+          // (a NaN among them: the row is NaN in any case)
+          const float m = fmaxf(ref[j], lane_greater<32>(lane_greater<16>(top[j])));
           const float shrink = m == kNone ? 1.f : __builtin_amdgcn_exp2f(ref[j] - m);
           l[j] *= shrink;
 #pragma unroll
@@ -424,6 +453,31 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
             for (int i = 0; i < 4; ++i) acc[j][c][i] *= shrink;
           ref[j] = m;
         }
+      }
+      // out^T += V^T P^T, 16 columns at a time: lane n of the operand is column n, its eight tokens
+      // 4 g .. 4 g + 3 of both tiles. The products of the first columns with a row tile's weights run
+      // beside the making of the next tile's.
+      const uint32_t token = 4 * kg + ((kn >> 1) & 3) + 16 * (kn >> 3);
+      constexpr int kFirst = R == 1 ? DW : DW / 2;
+      bf16x8 pt[R][PT], vt[DW];
+      const auto column = [&](int c) {
+        const u32x2 w = transposed(staged + code_place<D>(token, c) + 8 * (kn & 1));
+        u32x4 x;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float pow = of_tile(my_vp, b);
+          x[2 * b] = codes_times<false>(w[b], pow);
+          x[2 * b + 1] = codes_times<true>(w[b], pow);
+        }
+        vt[c] = __builtin_bit_cast(bf16x8, x);
+      };
+      const auto product = [&](int j, int c, int z) {
+        acc[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt[c], pt[j][z], acc[j][c], 0, 0, 0);
+      };
+#pragma unroll
+      for (int c = 0; c < kFirst; ++c) column(c);
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
         const float low = ref[j] == kNone ? 0.f : ref[j];
         float pv[8];
 #pragma unroll
@@ -434,27 +488,32 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
             pv[4 * b + i] = __builtin_amdgcn_exp2f(fmaf(sc[j][b][i], kf, off));
           l[j] = fmaf((pv[4 * b] + pv[4 * b + 1]) + (pv[4 * b + 2] + pv[4 * b + 3]), of_tile(my_vi, b), l[j]);
         }
-        split_terms<PT>(pv, pt[j]);
-      }
-      // out^T += V^T P^T, 16 columns at a time: lane n of the operand is column n, its eight tokens
-      // 4 g .. 4 g + 3 of both tiles
-      const uint32_t token = 4 * kg + ((kn >> 1) & 3) + 16 * (kn >> 3);
+        if constexpr (PT == 2) split_two(pv, pt[j]);
+        else split_terms<PT>(pv, pt[j]);
+        if (j > 0) {
 #pragma unroll
-      for (int c = 0; c < DW; ++c) {
-        const u32x2 w = transposed(staged + code_place<D>(token, c) + 8 * (kn & 1));
-        u32x4 vt;
+          for (int z = PT - 1; z >= 0; --z)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float pow = of_tile(my_vp, b);
-          vt[2 * b] = codes_times<false>(w[b], pow);
-          vt[2 * b + 1] = codes_times<true>(w[b], pow);
+            for (int c = 0; c < kFirst; ++c) product(j - 1, c, z);
+#pragma unroll
+          for (int x = 0; x < PT * kFirst; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int z = PT - 1; z >= 0; --z)
+#pragma unroll
+        for (int c = 0; c < kFirst; ++c) product(R - 1, c, z);
+#pragma unroll
+      for (int c = kFirst; c < DW; ++c) {
+        column(c);
 #pragma unroll
         for (int z = PT - 1; z >= 0; --z)
 #pragma unroll
-          for (int j = 0; j < R; ++j)
-            acc[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt), pt[j][z],
-                                                                acc[j][c], 0, 0, 0);
+          for (int j = 0; j < R; ++j) product(j, c, z);
       }
     };
 #pragma unroll
