@@ -20,6 +20,7 @@ struct RotateArgs {
   const int32_t* positions;
   int64_t n_tokens;
   double log2_base;
+  double between[8];     // of the launch: a lane's pairs, relative to its first one
   float eps;
 };
 

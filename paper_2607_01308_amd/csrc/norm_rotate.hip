@@ -11,6 +11,7 @@
 // pairs of either style are its own; d / (2 * elements of a piece) lanes share a row and sum its
 // squares within the wave. A wave takes several heads of one token, for which its angles are
 // the same.
+#include <cmath>
 #include <type_traits>
 
 #include "draft.h"
@@ -80,11 +81,13 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(RotateArgs a, int
   const int64_t waves = (int64_t)gridDim.x * (kThreads / 64);
   const int per = (groups + parts - 1) / parts;
   float qw[2][E], kw[2][E];
-  double freq[E];                        // revolutions a position, of the lane's pairs
+  // revolutions a position, of the lane's pairs: those of its first one times the powers of the base
+  // between them, which the host made (an exp2 in fp64 for each pair took as long as a token's heads)
+  double freq[E];
+  const double first = 0.15915494309189535 * exp2(-(2.0 / D) * (HALF ? c0 : c0 / 2) * a.log2_base);
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int i = HALF ? c0 + e : c0 / 2 + (e < E / 2 ? e : D / 4 + e - E / 2);
-    freq[e] = 0.15915494309189535 * exp2(-(2.0 / D) * i * a.log2_base);
+    freq[e] = first * a.between[e];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       qw[s][e] = weight_at(a.q, c0 + s * (D / 2) + e);
@@ -153,6 +156,9 @@ hipError_t launch_norm_rotate(RotateArgs a, int32_t d, int32_t dtype, int32_t st
     constexpr int ES = decltype(es)::value, D = decltype(dd)::value;
     constexpr bool HALF = decltype(half)::value;
     constexpr int kRows = 64 / (D / (2 * (16 / ES)));
+    constexpr int E = 16 / ES;
+    for (int e = 0; e < E; ++e)
+      a.between[e] = std::exp2(-(2.0 / D) * (HALF || e < E / 2 ? e : D / 4 + e - E / 2) * a.log2_base);
     const int32_t groups = (a.q.heads + a.k.heads + kRows - 1) / kRows;
     // a token's heads by as many waves as fill the GPU
     const int64_t fill = (int64_t)device_cu_count() * 16;
