@@ -22,6 +22,7 @@ namespace cm {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kGroups = 4;             // workgroups of a compute unit (126 registers a lane)
 
 template <int CTRL>
 __device__ __forceinline__ float moved(float x) {
@@ -63,15 +64,45 @@ __device__ __forceinline__ u32x4 pack(const float (&x)[16 / ES]) {
   return v;
 }
 
-__device__ __forceinline__ float weight_at(const HeadRows& r, int i) {
-  if (!r.weight) return 1.f;
-  if (r.weight_dtype == CM_F32) return static_cast<const float*>(r.weight)[i];
-  return __uint_as_float((uint32_t) static_cast<const uint16_t*>(r.weight)[i] << 16);
+// E weights from element i on (at any address of their type's), 1 where there are none.
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t words2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t half_words2 __attribute__((ext_vector_type(2), aligned(2)));
+template <int E>
+__device__ __forceinline__ void weights(const HeadRows& r, int i, float (&w)[E]) {
+#pragma unroll
+  for (int e = 0; e < E; ++e) w[e] = 1.f;
+  if (!r.weight) return;
+  if (r.weight_dtype == CM_F32) {
+#pragma unroll
+    for (int k = 0; k < E / 4; ++k) {
+      const words4 x = *(const CM_GLOBAL words4*)(global_ptr<float>(r.weight) + i + 4 * k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[4 * k + e] = __uint_as_float(x[e]);
+    }
+  } else {
+    const CM_GLOBAL uint16_t* at = global_ptr<uint16_t>(r.weight) + i;
+    uint32_t x[E / 2];
+    if constexpr (E == 8) {
+      const words2 y = *(const CM_GLOBAL words2*)at;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = y[k];
+    } else {
+      const half_words2 y = *(const CM_GLOBAL half_words2*)at;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) x[k] = y[k];
+    }
+#pragma unroll
+    for (int k = 0; k < E / 2; ++k) {
+      w[2 * k] = low_bf16(x[k]);
+      w[2 * k + 1] = high_bf16(x[k]);
+    }
+  }
 }
 
 // parts: waves that share a token's heads; groups: row groups of a wave's width that a token has.
 template <int ES, int D, bool HALF>
-__global__ __launch_bounds__(kThreads) void norm_rotate_kernel(RotateArgs a, int32_t parts,
+__global__ __launch_bounds__(kThreads, kGroups) void norm_rotate_kernel(RotateArgs a, int32_t parts,
                                                                int32_t groups, int64_t units) {
   constexpr int E = 16 / ES;             // elements of a piece
   constexpr int kLanes = D / (2 * E);    // lanes of a row
@@ -81,6 +112,11 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(RotateArgs a, int
   const int64_t waves = (int64_t)gridDim.x * (kThreads / 64);
   const int per = (groups + parts - 1) / parts;
   float qw[2][E], kw[2][E];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    weights(a.q, c0 + s * (D / 2), qw[s]);
+    weights(a.k, c0 + s * (D / 2), kw[s]);
+  }
   // revolutions a position, of the lane's pairs: those of its first one times the powers of the base
   // between them, which the host made (an exp2 in fp64 for each pair took as long as a token's heads)
   double freq[E];
@@ -88,11 +124,6 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(RotateArgs a, int
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     freq[e] = first * a.between[e];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      qw[s][e] = weight_at(a.q, c0 + s * (D / 2) + e);
-      kw[s][e] = weight_at(a.k, c0 + s * (D / 2) + e);
-    }
   }
   for (int64_t u = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6); u < units; u += waves) {
     const int64_t t = parts == 1 ? u : u / parts;
@@ -165,7 +196,7 @@ hipError_t launch_norm_rotate(RotateArgs a, int32_t d, int32_t dtype, int32_t st
     int32_t parts = (int32_t)(fill / a.n_tokens < 1 ? 1 : fill / a.n_tokens > groups ? groups : fill / a.n_tokens);
     const int32_t per = (groups + parts - 1) / parts;
     parts = (groups + per - 1) / per;
-    const int64_t units = a.n_tokens * parts, most = (int64_t)device_cu_count() * 8;
+    const int64_t units = a.n_tokens * parts, most = (int64_t)device_cu_count() * kGroups;
     const int64_t blocks = (units + kThreads / 64 - 1) / (kThreads / 64);
     ScopedTiming tm(K_NORM_ROTATE, stream);
     hipLaunchKernelGGL((norm_rotate_kernel<ES, D, HALF>), dim3((uint32_t)(blocks < most ? blocks : most)),
