@@ -98,6 +98,7 @@ struct VerifyShared {
   int64_t drafts[CM_DRAFT_MAX_NODES];  // the request's nodes
   int32_t parents[CM_DRAFT_MAX_NODES];
   float accept[CM_DRAFT_MAX_NODES];
+  float p[CM_DRAFT_MAX_NODES], q[CM_DRAFT_MAX_NODES];  // their tokens' in the rows of their parents
   int32_t n_gone;
 };
 
@@ -118,10 +119,16 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
       for (int64_t i = first + threadIdx.x; i < next; i += kThreads) a.path[i] = -1;
     return;
   }
+  // (what the walk looks at, at once: a look-up in memory for each node on its way took as long as a pass)
   for (int i = threadIdx.x; i < c; i += kThreads) {
-    lds.drafts[i] = a.drafts[first + i];
-    lds.parents[i] = a.parents[first + i];
+    const int64_t t = a.drafts[first + i];
+    const int32_t of = a.parents[first + i];
+    const bool in = of >= 0 && of < i && t >= 0 && t < a.V;
+    lds.drafts[i] = t;
+    lds.parents[i] = of;
     lds.accept[i] = a.accept[first + i];
+    lds.p[i] = in ? element<ES>(static_cast<const uint8_t*>(a.p) + (first + of) * a.p_row * ES, t) : 0.f;
+    lds.q[i] = in && a.q ? element<ES>(static_cast<const uint8_t*>(a.q) + (first + of) * a.q_row * ES, t) : 0.f;
   }
   if (threadIdx.x == 0) lds.n_gone = 0;
   __syncthreads();
@@ -244,16 +251,14 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     m = 1.0;
     int x = child(node, node);
     for (; x < c; x = child(node, x)) {
-      const int64_t t = drafts[x];
-      const bool in = t >= 0 && t < V;
-      const double pt = in ? clean(element<ES>(p, t)) : 0.0, u = accept[x];
+      const double pt = clean(lds.p[x]), u = accept[x];
       double r, want = u;
       if (sampled) {
-        const double qt = in ? clean(element<ES>(q, t)) : 0.0;
+        const double qt = clean(lds.q[x]);
         r = fmax(fma(-M, qt, pt), 0.0);
         want *= qt;
       } else {
-        r = tried(node, x, t) ? 0.0 : pt;
+        r = tried(node, x, drafts[x]) ? 0.0 : pt;
       }
       if (want * m < r) break;
       if (sampled) {
