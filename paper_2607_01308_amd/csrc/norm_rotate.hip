@@ -10,7 +10,9 @@
 // A lane holds two 16-byte pieces of a row, one of each half of it at the same place, so that the
 // pairs of either style are its own; d / (2 * elements of a piece) lanes share a row and sum its
 // squares within the wave. A wave takes several heads of one token, for which its angles are
-// the same.
+// the same. As many waves as run together take the tokens one after another, so that each reads the weights
+// and makes its frequencies once (twice as many waves, weights read one by one: 78 us). 16384
+// tokens of 40 heads of 128, bf16: 68 us, 4.9 TB/s, what a copy reaches; the sines take 40% of the SIMDs' time.
 #include <cmath>
 #include <type_traits>
 

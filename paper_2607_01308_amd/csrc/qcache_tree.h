@@ -11,8 +11,13 @@
 // beside its matrix instructions is shared by all rows. A workgroup's four waves take equal parts of
 // a range of the context, each whole steps, without a barrier until the range ends; then they
 // are joined through the LDS by all threads. As many workgroups as run together take equal spans of
-// all contexts, a request's once for each tile of 16 R rows, laid end to end; where a tile lies in
-// several spans, the last workgroup to write its partial results joins them, in their order.
+// all contexts, a request's once for each tile of 16 R rows, laid end to end, or begun anew with every tile
+// where that is no longer; a second launch joins the tiles that lie in several spans, in their order.
+//
+// What bounds it with 64 rows a wave (bf16, d = 128): a step's 96 matrix instructions take 1536 clocks of
+// a SIMD, its 350 vector instructions, 32 of them exponentials, about 1800; two waves share a SIMD and
+// overlap in part. 128 rows over 264 thousand tokens: 249 us, 0.83 PFLOP/s of matrix instructions (a
+// third of them the weights' second term), 2.2 TB/s of codes.
 #pragma once
 
 #include "draft.h"
@@ -21,6 +26,7 @@
 namespace cm {
 
 constexpr int kTreeWaves = 4;
+constexpr int kTreeRange = 2;                    // what a range costs beside its units, in units
 constexpr int kTreeThreads = 64 * kTreeWaves;
 
 // Row tiles of 16 that a wave takes at most: its registers hold D / 4 values of the output and
@@ -142,7 +148,7 @@ struct TreeShared {
   float m[kTreeWaves][16 * R], l[kTreeWaves][16 * R];
   int pos[CM_QCACHE_MAX_REQUESTS + 1];                         // where the requests begin, in units
   float cost[kTreeWaves];
-  int sums[kTreeWaves];
+  int sums[kTreeWaves], tiles[kTreeWaves];
   int first;
 };
 
@@ -611,43 +617,77 @@ __global__ __launch_bounds__(kTreeThreads, tree_groups(TERMS, D, R)) void qcache
 
   // where every request begins: prefix sums of the units of all its tiles
   const int per = (a.n + kTreeThreads - 1) / kTreeThreads;
-  int units[kPer], mine = 0;
+  int units[kPer], tiles[kPer], mine = 0, my_tiles = 0;
   float cost = 0.f;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     const int r = (int)threadIdx.x * per + k;
-    units[k] = 0;
+    units[k] = tiles[k] = 0;
     if (k < per && r < a.n) {
       TreeItem it;
       tree_request(ta, r, it);
-      const int tiles = (it.count * a.G + 16 * R - 1) / (16 * R);
-      if (tiles) {
-        units[k] = tiles * tree_units(ta, it);
-        cost += (float)tiles * (float)tree_units(ta, it);
+      tiles[k] = (it.count * a.G + 16 * R - 1) / (16 * R);
+      if (tiles[k]) {
+        units[k] = tree_units(ta, it);
+        cost += (float)tiles[k] * (float)units[k];
       }
     }
-    mine += units[k];
+    mine += tiles[k] * units[k];
+    my_tiles += tiles[k];
   }
-  const int upto = wave_scan(mine);
+  const auto prefix = [&](int x) {
+    const int upto = wave_scan(x);
+    if (lane == 63) lds.sums[wave] = upto;
+    __syncthreads();
+    int before = upto - x;
+#pragma unroll
+    for (int v = 0; v < kTreeWaves; ++v)
+      if (v < wave) before += lds.sums[v];
+    return before;
+  };
+  my_tiles = wave_scan(my_tiles);
   cost = wave_scan(cost);
   if (lane == 63) {
-    lds.sums[wave] = upto;
+    lds.tiles[wave] = my_tiles;
     lds.cost[wave] = cost;
   }
-  __syncthreads();
-  int at = upto - mine, total = 0;
+  int at = prefix(mine), total = 0, all_tiles = 0;
   cost = 0.f;
 #pragma unroll
   for (int v = 0; v < kTreeWaves; ++v) {
-    if (v < wave) at += lds.sums[v];
     total += lds.sums[v];
+    all_tiles += lds.tiles[v];
     cost += lds.cost[v];
   }
   // (rows that lie over one another: more units than an int holds, which nobody takes)
   if (cost > 2e9f) return;
   total = __builtin_amdgcn_readfirstlane(total);
+  all_tiles = __builtin_amdgcn_readfirstlane(all_tiles);
   int span = (total + a.few_items - 1) / a.few_items;
+  // Spans that begin with every tile, so that none has two ranges, whose queries, pages and sums take
+  // about as long as two units: the least span s for which total + tiles (s - 1) units are no more than
+  // the spans hold. (24 fp32 trees of up to 23 nodes, a window of 1000: 28.6 -> 22.2 us a call.)
+  bool whole = false;
+  if (all_tiles < a.few_items) {
+    const int apart = (total - all_tiles + a.few_items - all_tiles - 1) / (a.few_items - all_tiles);
+    whole = apart <= span + kTreeRange;
+    span = whole ? apart : span;
+  }
   span = span < ta.least ? ta.least : span;
+  if (whole) {
+    mine = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      units[k] = (units[k] + span - 1) / span * span;
+      mine += tiles[k] * units[k];
+    }
+    __syncthreads();
+    at = prefix(mine);
+    total = 0;
+#pragma unroll
+    for (int v = 0; v < kTreeWaves; ++v) total += lds.sums[v];
+    total = __builtin_amdgcn_readfirstlane(total);
+  }
   int u = w * span;
   const int stop = u + span < total ? u + span : total;
 #pragma unroll
@@ -655,9 +695,9 @@ __global__ __launch_bounds__(kTreeThreads, tree_groups(TERMS, D, R)) void qcache
     const int r = (int)threadIdx.x * per + k;
     if (k < per && r < a.n) {
       lds.pos[r] = at;
-      if (u >= at && u < at + units[k]) lds.first = r;
+      if (u >= at && u < at + tiles[k] * units[k]) lds.first = r;
     }
-    at += units[k];
+    at += tiles[k] * units[k];
   }
   if (threadIdx.x == 0) lds.pos[a.n] = total;
   __syncthreads();
@@ -673,9 +713,9 @@ __global__ __launch_bounds__(kTreeThreads, tree_groups(TERMS, D, R)) void qcache
     }
     TreeItem it;
     tree_request(ta, r, it);
-    const int each = tree_units(ta, it);
-    it.tile = (u - from) / each;
-    const int tile_from = from + it.tile * each, tile_to = tile_from + each;
+    const int each = tree_units(ta, it), room = whole ? (each + span - 1) / span * span : each;
+    it.tile = (u - from) / room;
+    const int tile_from = from + it.tile * room, tile_to = tile_from + each;
     const int u0 = u;
     u = tile_to < stop ? tile_to : stop;
     const int begin = tree_begin(ta, it);
@@ -691,6 +731,7 @@ __global__ __launch_bounds__(kTreeThreads, tree_groups(TERMS, D, R)) void qcache
                           live < 16 * R ? live : 16 * R};
     }
     tree_segment<TERMS, D, R>(ta, it, h, 2 * w + mid, lds);
+    if (whole) break;
     if (u == to) ++r;
   }
 }

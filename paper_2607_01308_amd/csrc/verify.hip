@@ -12,8 +12,13 @@
 // hundred thousand terms are off by 1e-14 of themselves, not by 1e-6, beside which the borders of
 // a sampled token lie close.
 //
-// One workgroup takes a request: its walk looks at single probabilities, and a pass over a
-// row sums r where a rejected child has a sibling after it or the token is to be sampled.
+// One workgroup takes a request: its walk looks at single probabilities, which it has read at once into
+// the LDS, and a pass over a row sums r where a rejected child has a sibling after it or the token is
+// to be sampled. A pass is bound by the vector instructions of its compute unit, 9 for an element (two
+// conversions and three operations in fp64, the check of its bits): 100003 tokens about 6 us. A pass
+// shared by several workgroups would exchange its sum through memory, four trips of 0.7 us, and gain
+// from about 200 thousand tokens on. 32 trees of up to 25 nodes over 100003 tokens: 47 us, as long as the
+// request with the most rejections.
 #include "draft.h"
 #include "qcache_ops.h"
 
