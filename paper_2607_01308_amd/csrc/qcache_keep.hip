@@ -71,18 +71,27 @@ __device__ __forceinline__ void keep_lengths(const KeepArgs& a) {
   __syncthreads();
   int64_t from[kPer], some[kPer], sum = 0;
   bool bad = false;
+  const int per = (a.n + kThreads - 1) / kThreads;  // requests of a thread
 #pragma unroll
   for (int x = 0; x < kPer; ++x) {
-    const int r = tid * kPer + x;
+    const int r = tid * per + x;
     from[x] = some[x] = 0;
-    if (r >= a.n) continue;
+    if (x >= per || r >= a.n) continue;
     const Kept k = kept_of(a, r);
     bad |= !k.good;
+    // (eight loads at a time: one after another the longest path bounds a small step)
+    const int kept = k.good ? k.kept : 0;
     int last = -1;
-    for (int i = 0; k.good && i < k.kept; ++i) {
-      const int p = a.path[k.row0 + i];
-      bad |= p <= last || p >= k.count;
-      last = p;
+    for (int i = 0; i < kept; i += 8) {
+      int p[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = a.path[k.row0 + (i + e < kept ? i + e : kept - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (i + e < kept) {
+          bad |= p[e] <= last || p[e] >= k.count;
+          last = p[e];
+        }
     }
     const int64_t t = a.lens[r] > 0 ? a.lens[r] : 0;
     const int64_t left = k.held + k.kept > 0 ? k.held + k.kept : 0;
@@ -110,7 +119,7 @@ __device__ __forceinline__ void keep_lengths(const KeepArgs& a) {
   }
 #pragma unroll
   for (int x = 0; x < kPer; ++x) {
-    const int32_t* row = a.table + (int64_t)(tid * kPer + x) * a.width;
+    const int32_t* row = a.table + (int64_t)(tid * per + x) * a.width;
     for (int64_t j = 0; j < some[x]; ++j)
       if (at + j < a.n_freed) a.freed[at + j] = row[from[x] + j];
     at += some[x];
