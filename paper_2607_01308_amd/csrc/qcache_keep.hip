@@ -19,6 +19,9 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
+// Slices of a head that a wave of cm_qcache_keep takes together: the chain of loads (rows, path, table, scales,
+// codes) is the same for all.
+constexpr int kUnits = 2;
 
 // A request's rows of the step as keep sees them.
 struct Kept {
@@ -140,11 +143,18 @@ __global__ __launch_bounds__(kThreads) void qcache_keep_kernel(KeepArgs a, int32
     return;
   }
   const int lane = threadIdx.x & 63;
-  const int unit = ((int)blockIdx.x - 1) * kWaves + (threadIdx.x >> 6);  // (layer, K/V, head)
-  if (unit >= units) return;
-  const int slice = unit / a.c.H, h = unit - slice * a.c.H;
-  float* scales = a.c.scales + slice * a.c.slice_scales() + h;
-  uint8_t* codes = a.c.codes + slice * a.c.slice_codes() + (((int64_t)h << a.c.b_shift) * D);
+  const int unit0 = (((int)blockIdx.x - 1) * kWaves + (threadIdx.x >> 6)) * kUnits;  // (layer, K/V, head)
+  if (unit0 >= units) return;
+  float* scales[kUnits];
+  uint8_t* codes[kUnits];
+  bool live[kUnits];
+#pragma unroll
+  for (int y = 0; y < kUnits; ++y) {
+    live[y] = unit0 + y < units;
+    const int unit = live[y] ? unit0 + y : unit0, slice = unit / a.c.H, h = unit - slice * a.c.H;
+    scales[y] = a.c.scales + slice * a.c.slice_scales() + h;
+    codes[y] = a.c.codes + slice * a.c.slice_codes() + (((int64_t)h << a.c.b_shift) * D);
+  }
   const int64_t page_codes = ((int64_t)a.c.H << a.c.b_shift) * D;
   const int B = 1 << a.c.b_shift;
   for (int r = blockIdx.y; r < a.n; r += gridDim.y) {
@@ -166,18 +176,22 @@ __global__ __launch_bounds__(kThreads) void qcache_keep_kernel(KeepArgs a, int32
       const int i0 = (int)(t - k.held), some = (int)(stop - t), begin = (int)(t & (B - 1));
       const int32_t page = table[t >> a.c.b_shift];
       const bool there = page >= 0 && page < a.c.pages;
-      const float own = there ? scales[(int64_t)page * a.c.H] : 0.f;
+      float own[kUnits], was[kUnits][2], top[kUnits];
+#pragma unroll
+      for (int y = 0; y < kUnits; ++y) {
+        own[y] = there ? scales[y][(int64_t)page * a.c.H] : 0.f;
+        top[y] = begin > 0 ? own[y] : 0.f;
+      }
       // where the rows come from: rows lane and lane + 64 of them
       int32_t from[2], at[2];
-      float was[2];
-      float top = begin > 0 ? own : 0.f;
       bool same = true;
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const int i = lane + 64 * x;
         from[x] = -1;
         at[x] = 0;
-        was[x] = 0.f;
+#pragma unroll
+        for (int y = 0; y < kUnits; ++y) was[y][x] = 0.f;
         if (i < some) {
           const int64_t s = k.held + path[i0 + i];
           const int32_t p = table[s >> a.c.b_shift];
@@ -186,36 +200,59 @@ __global__ __launch_bounds__(kThreads) void qcache_keep_kernel(KeepArgs a, int32
           const bool is = p >= 0 && p < a.c.pages;
           if (is) from[x] = p;
           // (a row that cannot come leaves the page's own scale among them)
-          was[x] = !is || p == page ? own : scales[(int64_t)p * a.c.H];
+#pragma unroll
+          for (int y = 0; y < kUnits; ++y)
+            was[y][x] = !is || p == page ? own[y] : scales[y][(int64_t)p * a.c.H];
         }
-        top = fmaxf(top, was[x]);
+#pragma unroll
+        for (int y = 0; y < kUnits; ++y) top[y] = fmaxf(top[y], was[y][x]);
       }
-      top = wave_max(top);
-      if (there && !(__all(same) && top == own)) {
-        uint8_t* to = codes + page * page_codes;
-        if (begin > 0 && top != own) {
-          const float ratio = ratio_of(own, top);
-          for (int u = lane; u < begin * kLanes; u += 64) {
-            u32x4* p = reinterpret_cast<u32x4*>(to) + u;
-            *p = rescaled(*p, ratio);
+      same = __all(same);
+      bool moves[kUnits], any = false;
+#pragma unroll
+      for (int y = 0; y < kUnits; ++y) {
+        top[y] = wave_max(top[y]);
+        moves[y] = live[y] && there && !(same && top[y] == own[y]);
+        any |= moves[y];
+      }
+      if (any) {
+        const int64_t to = page * page_codes;
+#pragma unroll
+        for (int y = 0; y < kUnits; ++y)
+          if (moves[y] && begin > 0 && top[y] != own[y]) {
+            const float ratio = ratio_of(own[y], top[y]);
+            for (int u = lane; u < begin * kLanes; u += 64) {
+              u32x4* p = reinterpret_cast<u32x4*>(codes[y] + to) + u;
+              *p = rescaled(*p, ratio);
+            }
           }
-        }
         for (int i = 0; i < some; i += kRows) {
           const int mine = i + lane / kLanes, look = mine & 63;
           const int32_t f0 = __shfl(from[0], look), f1 = __shfl(from[1], look);
           const int32_t a0 = __shfl(at[0], look), a1 = __shfl(at[1], look);
-          const float w0 = __shfl(was[0], look), w1 = __shfl(was[1], look);
           const int32_t f = mine < 64 ? f0 : f1;
           const int32_t row = mine < 64 ? a0 : a1;
-          const float w = mine < 64 ? w0 : w1;
+          float w[kUnits];
+#pragma unroll
+          for (int y = 0; y < kUnits; ++y) {
+            const float w0 = __shfl(was[y][0], look), w1 = __shfl(was[y][1], look);
+            w[y] = mine < 64 ? w0 : w1;
+          }
           if (mine < some && f >= 0) {
-            const u32x4 c = *reinterpret_cast<const u32x4*>(codes + f * page_codes + row * D +
-                                                            lane % kLanes * 16);
-            *reinterpret_cast<u32x4*>(to + (begin + mine) * D + lane % kLanes * 16) =
-                w == top ? c : rescaled(c, ratio_of(w, top));
+            u32x4 c[kUnits];
+#pragma unroll
+            for (int y = 0; y < kUnits; ++y)
+              c[y] = *global_ptr<u32x4>(codes[y] + f * page_codes + row * D + lane % kLanes * 16);
+#pragma unroll
+            for (int y = 0; y < kUnits; ++y)
+              if (moves[y])
+                *reinterpret_cast<u32x4*>(codes[y] + to + (begin + mine) * D + lane % kLanes * 16) =
+                    w[y] == top[y] ? c[y] : rescaled(c[y], ratio_of(w[y], top[y]));
           }
         }
-        if (lane == 0) scales[(int64_t)page * a.c.H] = top;
+#pragma unroll
+        for (int y = 0; y < kUnits; ++y)
+          if (moves[y] && lane == 0) scales[y][(int64_t)page * a.c.H] = top[y];
       }
       t = stop;
     }
@@ -256,7 +293,7 @@ __global__ __launch_bounds__(kThreads) void qcache_copy_kernel(QCacheDesc c, con
 
 hipError_t launch_qcache_keep(const KeepArgs& a, hipStream_t stream) {
   const int32_t units = 2 * a.c.L * a.c.H;       // (at most 65535)
-  const dim3 grid((uint32_t)(1 + (units + kWaves - 1) / kWaves), (uint32_t)a.n);
+  const dim3 grid((uint32_t)(1 + (units + kWaves * kUnits - 1) / (kWaves * kUnits)), (uint32_t)a.n);
   ScopedTiming tm(K_QCACHE_KEEP, stream);
   switch (a.c.d) {
     case 64: hipLaunchKernelGGL(qcache_keep_kernel<64>, grid, dim3(kThreads), 0, stream, a, units); break;
