@@ -49,6 +49,20 @@ def test_heads_of_one_projection(style, d, dtype, wtype):
     assert torch.equal(v, before[:, Hq + Hk:])
 
 
+@pytest.mark.parametrize("at", [1, 3, 7])
+@pytest.mark.parametrize("d", [64, 256])
+@pytest.mark.parametrize("dtype,wtype", [(BF16, BF16), (BF16, F32), (F32, F32), (F32, BF16)])
+def test_weights_at_any_address(dtype, wtype, d, at):
+    """Weights that begin anywhere in a tensor, with nothing of it behind them."""
+    q, k = values(5, 3, d, seed=d, dtype=dtype), values(5, 2, d, seed=d + 1, dtype=dtype)
+    positions = [3, 0, 70_000, 12, 9]
+    pos = torch.tensor(positions, dtype=torch.int32, device="cuda")
+    w = values(at + d, seed=at, dtype=wtype)[at:]
+    got = cm.norm_rotate(q, k, pos, 1e4, q_weight=w, k_weight=w)
+    check(q, got[0], positions, 1e4, "half", w)
+    check(k, got[1], positions, 1e4, "half", w)
+
+
 @pytest.mark.parametrize("T", [0, 1, 2, 63, 700, 9000])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_any_number_of_tokens(T, dtype):

@@ -173,6 +173,24 @@ def test_many_requests(n):
     check(q, codes, scales, 0, table, lens, counts, sees, positions)
 
 
+@pytest.mark.parametrize("longest", [100, 2500])
+@pytest.mark.parametrize("n", [3, 40, 63, 64, 90])
+def test_ranges_of_many_tiles(n, longest):
+    """Eight heads leave 64 workgroups for a head: fewer and more tiles than those, which begin with them
+    or anywhere, short ones of one range and long ones of several."""
+    rng = np.random.default_rng(n + longest)
+    counts = [int(x) for x in rng.integers(0, 4, size=n)]
+    lens = [c + int(x) for c, x in zip(counts, rng.integers(0, longest, size=n))]
+    lens[0], counts[1] = 8 * longest, 1
+    counts[0] = 3
+    lens[1] = 1
+    table, P = deal(lens, 32, seed=n)
+    codes, scales = filled(P, 8, 32, 64, seed=n)
+    sees, positions = seen(forest(counts, 2, seed=n), lens, 0)
+    q = queries(sum(counts), 8, 64, BF16, seed=n)
+    check(q, codes, scales, 0, table, lens, counts, sees, positions, device="cuda")
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_a_chain_is_causal(dtype):
     """A chain of nodes sees what the causal attention's rows see."""
