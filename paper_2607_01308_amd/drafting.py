@@ -27,9 +27,11 @@ def _heads(x: torch.Tensor, out: Optional[torch.Tensor], weight: Optional[torch.
         raise TypeError(f"q and k must both be bfloat16 or float32, got {x.dtype}")
     if x.device != device:
         raise ValueError(f"{name} must live on {device}, got {x.device}")
-    if out is None:
+    if out is None and stream is None:
+        out = x.new_empty(x.shape)
+    elif out is None:
         with _made_on(stream):
-            out = torch.empty(x.shape, dtype=dtype, device=device)
+            out = x.new_empty(x.shape)
     elif out.shape != x.shape or out.dtype is not dtype or out.device != device:
         raise ValueError(f"{name}_out must have {name}'s shape, type and device")
     if x.stride(2) != 1 or out.stride(2) != 1:
@@ -63,13 +65,14 @@ def norm_rotate(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Ten
     if not q.is_cuda:
         raise ValueError("q must live on a GPU")
     _check(positions, "positions", torch.int32, dev, (tokens,))
+    given = q_out, k_out
     q_out, qr = _heads(q, q_out, q_weight, "q", dev, tokens, d, q.dtype, stream)
     kr = None
     if k is not None:
         k_out, kr = _heads(k, k_out, k_weight, "k", dev, tokens, d, q.dtype, stream)
     elif k_out is not None or k_weight is not None:
         raise ValueError("k_out and k_weight need k")
-    s, here = _use(stream, dev, q, k, positions, q_weight, k_weight, q_out, k_out)
+    s, here = _use(stream, dev, q, k, positions, q_weight, k_weight, *given)
     rope = C.CmRope(base=float(rope_base), style=_STYLES[style], reserved=0)
     C.check(_call(here, dev, C.lib().cm_norm_rotate, d, _DTYPES[q.dtype], tokens, positions.data_ptr(),
                   ctypes.byref(rope), eps, ctypes.byref(qr), None if kr is None else ctypes.byref(kr),
