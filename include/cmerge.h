@@ -734,7 +734,13 @@ typedef struct {
   int32_t* path_dev;               /* n_rows */
   int32_t* counts_dev;             /* n */
   int64_t* tokens_dev;             /* n */
+  void* workspace;                 /* cm_verify_drafts_size() bytes, 256-byte aligned, or NULL */
+  size_t workspace_bytes;
 } cm_drafts;
+/* Workspace (from n, dtype and vocabulary): with it several workgroups share a request's passes over a
+ * row, and the results are the same. It must be zero before its first use and is used for nothing else; a call leaves
+ * it zero. Calls that may overlap have workspaces of their own. 0 bytes where it would not help. */
+int32_t cm_verify_drafts_size(const cm_drafts* drafts, size_t* bytes_out);
 int32_t cm_verify_drafts(const cm_drafts* drafts, void* stream);
 
 /* What a step leaves in the cache: of request r the first counts_dev[r] entries of path_dev at its

@@ -40,7 +40,7 @@ EXPORTS = (
     "cm_paged_workspace_size", "cm_paged_order", "cm_paged_hash_select", "cm_paged_tables",
     "cm_paged_render", "cm_paged_render_hash", "cm_paged_deliveries",
     "cm_qcache_tables", "cm_qcache_write", "cm_qcache_attention_size", "cm_qcache_attention",
-    "cm_norm_rotate", "cm_verify_drafts", "cm_qcache_keep", "cm_qcache_copy",
+    "cm_norm_rotate", "cm_verify_drafts_size", "cm_verify_drafts", "cm_qcache_keep", "cm_qcache_copy",
     "cm_qcache_tree", "cm_qcache_tree_attention_size", "cm_qcache_tree_attention",
     "cm_timing_enable", "cm_timing_reset", "cm_timing_query",
 )
@@ -165,6 +165,8 @@ class CmDrafts(ctypes.Structure):
         ("path_dev", ctypes.c_void_p),
         ("counts_dev", ctypes.c_void_p),
         ("tokens_dev", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_size_t),
     ]
 
 
@@ -254,6 +256,7 @@ def lib() -> ctypes.CDLL:
             "cm_qcache_tree": (I32, [I32, I64, P, P, P, I32, I32, P, P, P, P]),
             "cm_qcache_tree_attention_size": (I32, [QC, QA, ctypes.POINTER(SZ)]),
             "cm_qcache_tree_attention": (I32, [QC, I32, QA, ctypes.POINTER(CmQtree), P, SZ, P]),
+            "cm_verify_drafts_size": (I32, [ctypes.POINTER(CmDrafts), ctypes.POINTER(ctypes.c_size_t)]),
             "cm_verify_drafts": (I32, [ctypes.POINTER(CmDrafts), P]),
             "cm_qcache_keep": (I32, [QC, ctypes.POINTER(CmQkeep), P]),
             "cm_qcache_copy": (I32, [QC, I32, I32, I64, P, P, P]),

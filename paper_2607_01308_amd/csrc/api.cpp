@@ -1511,6 +1511,19 @@ int32_t check_head_rows(const char* what, const cm_head_rows* r, int64_t n_token
   return CM_OK;
 }
 
+int32_t check_drafts_shape(const cm_drafts* s) {
+  int32_t st = CM_OK, esize = 0;
+  if (s->n < 1 || s->n > CM_QCACHE_MAX_REQUESTS)
+    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
+                               "], got " + std::to_string(s->n));
+  if ((st = element_bytes(s->dtype, &esize)) != CM_OK) return st;
+  if (s->n_rows < 0 || s->n_rows > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "n_rows must be in [0, 2^31), got " + std::to_string(s->n_rows));
+  if (s->vocabulary < 1 || s->vocabulary > 0x7FFFFFFF)
+    return fail(CM_EINVAL, "vocabulary must be in [1, 2^31), got " + std::to_string(s->vocabulary));
+  return CM_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1626,18 +1639,22 @@ int32_t cm_qcache_tree_attention(const cm_qcache* cache, int32_t layer, const cm
   return e == hipSuccess ? CM_OK : fail_hip(e, "cm_qcache_tree_attention");
 }
 
+int32_t cm_verify_drafts_size(const cm_drafts* s, size_t* bytes_out) {
+  g_err.clear();
+  if (!s) return fail(CM_EINVAL, "drafts is NULL");
+  if (!bytes_out) return fail(CM_EINVAL, "bytes_out is NULL");
+  int32_t st = check_drafts_shape(s);
+  if (st != CM_OK) return st;
+  *bytes_out = cm::verify_workspace(s->n, s->vocabulary);
+  return CM_OK;
+}
+
 int32_t cm_verify_drafts(const cm_drafts* s, void* stream) {
   g_err.clear();
   int32_t st = CM_OK, esize = 0;
   if (!s) return fail(CM_EINVAL, "drafts is NULL");
-  if (s->n < 1 || s->n > CM_QCACHE_MAX_REQUESTS)
-    return fail(CM_EINVAL, "n must be in [1, " + std::to_string(CM_QCACHE_MAX_REQUESTS) +
-                               "], got " + std::to_string(s->n));
-  if ((st = element_bytes(s->dtype, &esize)) != CM_OK) return st;
-  if (s->n_rows < 0 || s->n_rows > 0x7FFFFFFF)
-    return fail(CM_EINVAL, "n_rows must be in [0, 2^31), got " + std::to_string(s->n_rows));
-  if (s->vocabulary < 1 || s->vocabulary > 0x7FFFFFFF)
-    return fail(CM_EINVAL, "vocabulary must be in [1, 2^31), got " + std::to_string(s->vocabulary));
+  if ((st = check_drafts_shape(s)) != CM_OK) return st;
+  esize = s->dtype == CM_F32 ? 4 : 2;
   if (!s->rows_dev || !aligned(s->rows_dev, 4)) return fail(CM_EINVAL, "rows_dev is NULL or misaligned");
   if (!s->counts_dev || !aligned(s->counts_dev, 4))
     return fail(CM_EINVAL, "counts_dev is NULL or misaligned");
@@ -1661,7 +1678,11 @@ int32_t cm_verify_drafts(const cm_drafts* s, void* stream) {
       return fail(CM_EINVAL, "accept_dev is NULL or misaligned");
     if (!s->path_dev || !aligned(s->path_dev, 4)) return fail(CM_EINVAL, "path_dev is NULL or misaligned");
   }
+  if (s->workspace &&
+      (st = check_ws(s->workspace, s->workspace_bytes, cm::verify_workspace(s->n, s->vocabulary))) != CM_OK)
+    return st;
   cm::VerifyArgs a;
+  a.talk = s->workspace;
   a.n = s->n;
   a.n_rows = s->n_rows;
   a.V = s->vocabulary;

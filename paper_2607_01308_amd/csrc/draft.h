@@ -89,7 +89,10 @@ struct VerifyArgs {
   int32_t* path;
   int32_t* counts;
   int64_t* tokens;
+  void* talk;              // verify_workspace() bytes, or nullptr: one workgroup a request
+  int32_t groups;          // of the launch: workgroups of a request
 };
-hipError_t launch_verify_drafts(const VerifyArgs& a, int32_t dtype, hipStream_t stream);
+size_t verify_workspace(int32_t n, int64_t V);
+hipError_t launch_verify_drafts(VerifyArgs a, int32_t dtype, hipStream_t stream);
 
 }  // namespace cm

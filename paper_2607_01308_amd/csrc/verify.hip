@@ -26,11 +26,18 @@ namespace cm {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / 64;
+constexpr int kGroups = 2;           // workgroups of a compute unit
+constexpr int kParts = 64;           // parts of a row at most
+constexpr int64_t kPart = 8192;      // elements of one, or a multiple
 constexpr int kVec = 8;              // elements of a lane's load
 constexpr int kStep = 64 * kVec;     // and of a wave's
-constexpr int kBatch = 3;            // steps whose loads are under way together
+// How long a workgroup waits for another one, in ticks of 10 ns for each kPart elements of a part: a helper
+// for a pass, the first one for the helpers' sums. Neither is needed: a helper that has waited this long
+// ends, and the first one makes the sums itself.
+constexpr uint64_t kHelperWait = 100000;
+constexpr uint64_t kSumsWait = 20000;
 
 // What is not a probability counts as none.
 __device__ __forceinline__ double clean(float x) {
@@ -95,8 +102,35 @@ __device__ __forceinline__ uint32_t greatest_bits(uint32_t top, const float (&x)
   return top;
 }
 
+// What the workgroups of a request tell one another, all zero between calls. Words are stored and loaded
+// one by one, in no order; a reader takes them when the last one fits the others.
+struct VerifyTalk {
+  uint64_t pass[3];                    // the first one's: M's bits, the pass, both mixed
+  uint64_t left;                       // workgroups that are done
+  struct { uint64_t sum, mixed; } part[kParts];
+};
+__device__ __forceinline__ void tell(uint64_t* at, uint64_t x) {
+  __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t told(const uint64_t* at) {
+  return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// Bits that two passes, or two parts of one, share by chance alone; never 0.
+__device__ __forceinline__ uint64_t mark(uint64_t x) {
+  x = (x + 1) * 0x9E3779B97F4A7C15ull;
+  x = (x ^ (x >> 29)) * 0xBF58476D1CE4E5B9ull;
+  return (x ^ (x >> 32)) | 1;
+}
+// A pass: its number in the call, whether drafted tokens are taken out, the node.
+constexpr uint64_t kOver = 0x3FFFFFFF;
+__device__ __forceinline__ uint64_t pass_of(uint32_t number, bool gone, uint32_t node) {
+  return (uint64_t)number << 32 | (uint64_t)gone << 31 | node;
+}
+
 struct VerifyShared {
-  double part[kWaves];                 // sums of the waves' parts of the row
+  double part[kParts];                 // sums of the parts of the row
+  double waves[kParts][kWaves];        // and of the waves' shares of them
+  uint64_t missing, pass, M;
   double sub[kWaves];                  // and of their steps
   int64_t hit[kWaves], any[kWaves];
   int64_t gone[CM_DRAFT_MAX_NODES];    // tokens taken out of r
@@ -107,15 +141,18 @@ struct VerifyShared {
   int32_t n_gone;
 };
 
+// The first n workgroups take a request each; of the others every n-th helps one: it sums its parts of the
+// row in the passes that it is told of. A part's sum is the same whoever makes it.
 template <int ES>
-__global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
+__global__ __launch_bounds__(kThreads, kGroups * kWaves / 4) void verify_kernel(VerifyArgs a) {
   __shared__ VerifyShared lds;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int req = blockIdx.x;
+  const int req = blockIdx.x % a.n, mine = blockIdx.x / a.n;
   const int64_t first = a.rows[req], next = a.rows[req + 1];
   const bool fits = first >= 0 && next >= first && next <= a.n_rows;
   const int c = fits && next - first <= CM_DRAFT_MAX_NODES ? (int)(next - first) : 0;
   if (c == 0) {
+    if (mine > 0) return;
     if (threadIdx.x == 0) {
       a.counts[req] = 0;
       a.tokens[req] = -1;
@@ -124,6 +161,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
       for (int64_t i = first + threadIdx.x; i < next; i += kThreads) a.path[i] = -1;
     return;
   }
+  VerifyTalk* talk = static_cast<VerifyTalk*>(a.talk) + req;
   // (what the walk looks at, at once: a look-up in memory for each node on its way took as long as a pass)
   for (int i = threadIdx.x; i < c; i += kThreads) {
     const int64_t t = a.drafts[first + i];
@@ -164,8 +202,9 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
   const uint8_t *p = nullptr, *q = nullptr;
   const int64_t V = a.V;
   const bool sampled = a.q != nullptr;
-  // A wave's part of the row: whole steps.
-  const int64_t part = ((V + kWaves - 1) / kWaves + kStep - 1) / kStep * kStep;
+  // parts of the row, and a wave's share of one: whole steps
+  const int64_t part = (V + kParts * kPart - 1) / (kParts * kPart) * kPart, share = part / kWaves;
+  const int parts = (int)((V + part - 1) / part);
 
   // r of kVec elements, from v on, with the probabilities x and y
   const auto rest_of = [&](float (&x)[kVec], float (&y)[kVec], int64_t v, double M, double (&r)[kVec]) {
@@ -209,40 +248,160 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     for (int by = 1; by < 64; by <<= 1) x += __shfl_xor(x, by);
     return x;
   };
-  // sum r over the row; the waves' parts stay in lds.part
-  const auto total = [&](double M) {
-    double s = 0.0;
-    const int64_t begin = wave * part, end = begin + part < V ? begin + part : V;
-    int64_t v0 = begin;
-    for (; v0 + kBatch * kStep <= end; v0 += kBatch * kStep) {
-      Raw<ES> x[kBatch], y[kBatch];
+  // sums of the wave's shares of parts from, from + step, ..
+  const auto sum_parts = [&](int from, int step, double M) {
+    for (int i = from; i < parts; i += step) {
+      double s = 0.0;
+      const int64_t begin = i * part + wave * share, end = begin + share < V ? begin + share : V;
+      int64_t v0 = begin;
+      for (; v0 + 2 * kStep <= end; v0 += 2 * kStep) {
+        Raw<ES> x[2], y[2];
 #pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        x[b] = load_raw<ES>(p, v0 + b * kStep + lane * kVec);
-        if (sampled) y[b] = load_raw<ES>(q, v0 + b * kStep + lane * kVec);
+        for (int b = 0; b < 2; ++b) {
+          x[b] = load_raw<ES>(p, v0 + b * kStep + lane * kVec);
+          if (sampled) y[b] = load_raw<ES>(q, v0 + b * kStep + lane * kVec);
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          float xs[kVec], ys[kVec];
+          double r[kVec];
+          unpack<ES>(x[b], xs);
+          if (sampled) unpack<ES>(y[b], ys);
+          rest_of(xs, ys, v0 + b * kStep + lane * kVec, M, r);
+          s += sum_of(r);
+        }
       }
-#pragma unroll
-      for (int b = 0; b < kBatch; ++b) {
-        float xs[kVec], ys[kVec];
+      for (int64_t v = v0 + lane * kVec; v < end; v += kStep) {
         double r[kVec];
-        unpack<ES>(x[b], xs);
-        if (sampled) unpack<ES>(y[b], ys);
-        rest_of(xs, ys, v0 + b * kStep + lane * kVec, M, r);
+        rest(v, M, r);
         s += sum_of(r);
       }
+      s = wave_sum(s);
+      if (lane == 0) lds.waves[i][wave] = s;
     }
-    for (int64_t v = v0 + lane * kVec; v < end; v += kStep) {
-      double r[kVec];
-      rest(v, M, r);
-      s += sum_of(r);
-    }
-    s = wave_sum(s);
+  };
+  // The sum of part i, from its waves' (behind a barrier).
+  const auto part_sum = [&](int i) {
+    double s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) s += lds.waves[i][w];
+    return s;
+  };
+  // The tokens that children of node `of` drafted, taken out of r.
+  const auto take_out = [&](int of) {
     __syncthreads();
-    if (lane == 0) lds.part[wave] = s;
+    if (threadIdx.x == 0) lds.n_gone = 0;
+    __syncthreads();
+    for (int i = of + 1 + (int)threadIdx.x; i < c; i += kThreads)
+      if (parents[i] == of) lds.gone[atomicAdd(&lds.n_gone, 1)] = drafts[i];
+    __syncthreads();
+  };
+  // Done with the request's talk: the last one clears it.
+  const auto leave = [&] {
+    if (threadIdx.x != 0) return;
+    if (__hip_atomic_fetch_add(&talk->left, 1ull, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) !=
+        (uint64_t)a.groups - 1)
+      return;
+    for (int i = 0; i < 3; ++i) tell(&talk->pass[i], 0);
+    for (int i = 0; i < parts; ++i) {
+      tell(&talk->part[i].sum, 0);
+      tell(&talk->part[i].mixed, 0);
+    }
+    tell(&talk->left, 0);
+  };
+
+  if (mine > 0) {
+    uint32_t done = 0;
+    while (true) {
+      if (threadIdx.x == 0) {
+        const uint64_t start = wall_clock64();
+        uint64_t M, pass;
+        while (true) {
+          M = told(&talk->pass[0]);
+          pass = told(&talk->pass[1]);
+          const bool whole = told(&talk->pass[2]) == (M ^ mark(pass));
+          if (whole && (uint32_t)(pass >> 32) > done) break;
+          if (wall_clock64() - start > kHelperWait * (uint64_t)(part / kPart)) {
+            pass = kOver;
+            break;
+          }
+          __builtin_amdgcn_s_sleep(1);
+        }
+        lds.M = M;
+        lds.pass = pass;
+      }
+      __syncthreads();
+      const uint64_t pass = lds.pass;
+      const double M = __longlong_as_double((long long)lds.M);
+      const uint32_t node = (uint32_t)pass & 0x7FFFFFFFu;
+      if (node >= (uint32_t)c) break;            // (kOver)
+      done = (uint32_t)(pass >> 32);
+      p = static_cast<const uint8_t*>(a.p) + (first + node) * a.p_row * ES;
+      if (sampled) q = static_cast<const uint8_t*>(a.q) + (first + node) * a.q_row * ES;
+      if ((pass >> 31) & 1) take_out((int)node);
+      else if (threadIdx.x == 0) lds.n_gone = 0;
+      __syncthreads();
+      sum_parts(mine, a.groups, M);
+      __syncthreads();
+      if (threadIdx.x == 0)
+        for (int i = mine; i < parts; i += a.groups) {
+          const uint64_t x = (uint64_t)__double_as_longlong(part_sum(i));
+          tell(&talk->part[i].sum, x);
+          tell(&talk->part[i].mixed, x ^ mark(pass * kParts + i));
+        }
+    }
+    leave();
+    return;
+  }
+
+  // sum r over the row of `node`; the parts' sums stay in lds.part
+  uint32_t passes = 0;
+  int helpers = a.groups;
+  const auto tell_pass = [&](double M, uint64_t pass) {
+    if (threadIdx.x != 0) return;
+    const uint64_t x = (uint64_t)__double_as_longlong(M);
+    tell(&talk->pass[0], x);
+    tell(&talk->pass[1], pass);
+    tell(&talk->pass[2], x ^ mark(pass));
+  };
+  const auto total = [&](double M) {
+    const uint64_t pass = pass_of(++passes, !sampled && lds.n_gone > 0, (uint32_t)node);
+    __syncthreads();                             // (the sums before are not needed now)
+    if (helpers > 1) tell_pass(M, pass);
+    sum_parts(0, helpers, M);
+    __syncthreads();
+    for (int i = (int)threadIdx.x * helpers; i < parts; i += kThreads * helpers) lds.part[i] = part_sum(i);
+    if (helpers > 1) {
+      if (wave == 0) {
+        const uint64_t start = wall_clock64();
+        bool wants = lane < parts && lane % helpers != 0;
+        while (true) {
+          if (wants) {
+            const uint64_t x = told(&talk->part[lane].sum);
+            if (told(&talk->part[lane].mixed) == (x ^ mark(pass * kParts + lane))) {
+              lds.part[lane] = __longlong_as_double((long long)x);
+              wants = false;
+            }
+          }
+          if (!__any(wants) || wall_clock64() - start > kSumsWait * (uint64_t)(part / kPart)) break;
+        }
+        const uint64_t missing = __ballot(wants);
+        if (lane == 0) lds.missing = missing;
+      }
+      __syncthreads();
+      const uint64_t missing = lds.missing;
+      if (missing) {                             // (none of them is waited for again)
+        helpers = 1;
+        for (int i = 0; i < parts; ++i)
+          if ((missing >> i) & 1) sum_parts(i, kParts, M);
+        __syncthreads();
+        for (int i = threadIdx.x; i < parts; i += kThreads)
+          if ((missing >> i) & 1) lds.part[i] = part_sum(i);
+      }
+    }
     __syncthreads();
     double all = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) all += lds.part[w];
+    for (int i = 0; i < parts; ++i) all += lds.part[i];
     return all;
   };
 
@@ -279,12 +438,7 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
   for (int i = count + (int)threadIdx.x; i < c; i += kThreads) path[i] = -1;
 
   // the token after `node`
-  if (!sampled) {
-    __syncthreads();
-    for (int i = node + 1 + (int)threadIdx.x; i < c; i += kThreads)
-      if (parents[i] == node) lds.gone[atomicAdd(&lds.n_gone, 1)] = drafts[i];
-    __syncthreads();
-  }
+  if (!sampled) take_out(node);
   double all = total(M);
   if (!(all > 0.0)) {                            // nothing is left: as if no child had been tried
     M = 0.0;
@@ -293,13 +447,16 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
     __syncthreads();
     all = total(M);
   }
+  if (a.groups > 1) {
+    tell_pass(0.0, pass_of(passes + 1, false, (uint32_t)kOver));
+    leave();
+  }
   const double want = (double)a.sample[req] * all;
-  // the first wave's part that passes it, else the last that holds anything
+  // the first part that passes it, else the last that holds anything
   int w0 = -1;
   double before = 0.0, run = 0.0, before_last = 0.0;
   int last = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
+  for (int w = 0; w < parts; ++w) {
     if (lds.part[w] > 0.0) {
       last = w;
       before_last = run;
@@ -371,12 +528,24 @@ __global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
 
 }  // namespace
 
-hipError_t launch_verify_drafts(const VerifyArgs& a, int32_t dtype, hipStream_t stream) {
+// Workgroups of a request: as many as run together, none without a part of the row.
+int32_t verify_groups(int32_t n, int64_t V) {
+  const int64_t part = (V + kParts * kPart - 1) / (kParts * kPart) * kPart, parts = (V + part - 1) / part;
+  const int64_t groups = (int64_t)kGroups * device_cu_count() / n;
+  return (int32_t)(groups < 1 ? 1 : groups > parts ? parts : groups);
+}
+size_t verify_workspace(int32_t n, int64_t V) {
+  return verify_groups(n, V) > 1 ? sizeof(VerifyTalk) * (size_t)n : 0;
+}
+
+hipError_t launch_verify_drafts(VerifyArgs a, int32_t dtype, hipStream_t stream) {
+  a.groups = a.talk ? verify_groups(a.n, a.V) : 1;
+  const dim3 grid((uint32_t)(a.n * a.groups));
   ScopedTiming tm(K_VERIFY_DRAFTS, stream);
   if (dtype == CM_BF16)
-    hipLaunchKernelGGL(verify_kernel<2>, dim3((uint32_t)a.n), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(verify_kernel<2>, grid, dim3(kThreads), 0, stream, a);
   else
-    hipLaunchKernelGGL(verify_kernel<4>, dim3((uint32_t)a.n), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(verify_kernel<4>, grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -15,7 +15,7 @@ import torch
 
 from . import _cabi as C
 from .binding import _DTYPES, _STYLES
-from .qcache import QCache, _attention, _attention_step, _call, _check, _made_on, _use
+from .qcache import _WS, QCache, _attention, _attention_step, _call, _check, _made_on, _use
 
 
 def _heads(x: torch.Tensor, out: Optional[torch.Tensor], weight: Optional[torch.Tensor], name: str,
@@ -208,9 +208,28 @@ def verify_drafts(probs: torch.Tensor, drafts: torch.Tensor, parents: torch.Tens
                       parents.data_ptr(), rows.data_ptr(), accept.data_ptr(), sample.data_ptr(),
                       out.path.data_ptr(), out.counts.data_ptr(), out.tokens.data_ptr())
     s, here = _use(stream, dev, probs, draft_probs, drafts, parents, rows, accept, sample)
-    C.check(_call(here, dev, C.lib().cm_verify_drafts, ctypes.byref(step), s.cuda_stream),
-            "cm_verify_drafts")
+    with _made_on(None if stream is None and here else s):
+        ws = _verify_workspace(step, dev, s)
+        if ws is not None:
+            step.workspace, step.workspace_bytes = ws.data_ptr(), ws.numel()
+        C.check(C.lib().cm_verify_drafts(ctypes.byref(step), s.cuda_stream), "cm_verify_drafts")
     return out
+
+
+def _verify_workspace(step: C.CmDrafts, dev, s) -> Optional[torch.Tensor]:
+    """Zeros for a call on s, the current stream; kept as the attention's scratch is."""
+    need = ctypes.c_size_t(0)
+    C.check(C.lib().cm_verify_drafts_size(ctypes.byref(step), ctypes.byref(need)), "cm_verify_drafts_size")
+    if need.value == 0:
+        return None
+    capturing = torch.cuda.is_current_stream_capturing()
+    key = (dev, s.cuda_stream, "cm_verify_drafts")
+    ws = None if capturing else _WS.get(key)
+    if ws is None or ws.numel() < need.value:
+        ws = torch.zeros(need.value, dtype=torch.uint8, device=dev)
+        if not capturing:
+            _WS[key] = ws
+    return ws
 
 
 @dataclass

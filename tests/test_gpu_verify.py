@@ -1,12 +1,15 @@
 """Verification of drafted tokens (verify_drafts) on the GPU: accepted nodes and sampled tokens are
 those of a walk in 64 bits (tests/draft_ref.py)."""
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 import draft_ref as ref
 import paper_2607_01308_amd as cm
+from paper_2607_01308_amd import _cabi as C
 
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
@@ -220,3 +223,63 @@ def test_another_stream_and_a_graph():
         want = cm.verify_drafts(*tensors, draft_probs=c["draft_probs"])
         for a, b in ((got.path, want.path), (got.counts, want.counts), (got.tokens, want.tokens)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("sampled", [True, False])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,V", [(1, 200_003), (3, 100_001), (40, 30_000), (1, 600_000)])
+def test_shared_and_alone(n, V, dtype, sampled):
+    """Requests that several workgroups share have the results that one workgroup gives them, call after
+    call, and leave the workspace zero."""
+    c = case([int(x) for x in np.random.default_rng(V).integers(4, 12, size=n)], V, 3, dtype, sampled, seed=V)
+    if not sampled:                                      # (drafts that are likely: some are accepted)
+        c["probs"][:, :4] *= V / 8
+    check(c)
+    i32 = dict(dtype=torch.int32, device="cuda")
+    parents, rows = torch.tensor(c["parents"], **i32), torch.tensor(c["rows"], **i32)
+    u, s = torch.tensor(c["accept"], device="cuda"), torch.tensor(c["sample"], device="cuda")
+    many = [cm.verify_drafts(c["probs"], c["drafts"], parents, rows, u, s, draft_probs=c["draft_probs"])
+            for _ in range(8)]
+    T, q = len(c["parents"]), c["draft_probs"]
+    path, counts, tokens = torch.empty(T, **i32), torch.empty(n, **i32), torch.empty(n, dtype=torch.int64, device="cuda")
+    step = C.CmDrafts(n, C.CM_BF16 if dtype is BF16 else C.CM_F32, T, V, c["probs"].data_ptr(), V,
+                      None if q is None else q.data_ptr(), V, c["drafts"].data_ptr(), parents.data_ptr(),
+                      rows.data_ptr(), u.data_ptr(), s.data_ptr(), path.data_ptr(), counts.data_ptr(),
+                      tokens.data_ptr())
+    stream = torch.cuda.current_stream().cuda_stream
+    assert C.lib().cm_verify_drafts(ctypes.byref(step), stream) == C.CM_OK
+    for got in many:
+        assert torch.equal(got.path, path) and torch.equal(got.counts, counts) and torch.equal(got.tokens, tokens)
+    need = ctypes.c_size_t(0)
+    assert C.lib().cm_verify_drafts_size(ctypes.byref(step), ctypes.byref(need)) == C.CM_OK and need.value > 0
+    ws = torch.zeros(need.value, dtype=torch.uint8, device="cuda")
+    step.workspace, step.workspace_bytes = ws.data_ptr(), need.value - 1
+    assert C.lib().cm_verify_drafts(ctypes.byref(step), stream) == C.CM_EWORKSPACE
+    step.workspace_bytes = need.value
+    for x in (path, counts, tokens):
+        x.fill_(-7)
+    assert C.lib().cm_verify_drafts(ctypes.byref(step), stream) == C.CM_OK
+    assert torch.equal(tokens, many[0].tokens) and torch.equal(path, many[0].path)
+    assert not bool(ws.any())
+
+
+def test_shared_on_two_streams_and_in_a_graph():
+    """Calls on two streams at once, and a graph replayed beside them, have workspaces of their own."""
+    cases = [case([9, 5], 150_001, 3, BF16, True, seed=s) for s in (21, 22)]
+    i32 = dict(dtype=torch.int32, device="cuda")
+    args = [(c["probs"], c["drafts"], torch.tensor(c["parents"], **i32), torch.tensor(c["rows"], **i32),
+             torch.tensor(c["accept"], device="cuda"), torch.tensor(c["sample"], device="cuda"), c["draft_probs"])
+            for c in cases]
+    want = [cm.verify_drafts(*a) for a in args]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        inside = cm.verify_drafts(*args[0])
+    streams = [torch.cuda.Stream() for _ in args]
+    for _ in range(6):
+        inside.tokens.fill_(-5)
+        graph.replay()
+        got = [cm.verify_drafts(*a, stream=s) for a, s in zip(args, streams)]
+        torch.cuda.synchronize()
+        for g, w in zip(got + [inside], want + [want[0]]):
+            assert torch.equal(g.tokens, w.tokens) and torch.equal(g.path, w.path) and torch.equal(g.counts, w.counts)
