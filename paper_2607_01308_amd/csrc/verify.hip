@@ -12,13 +12,13 @@
 // hundred thousand terms are off by 1e-14 of themselves, not by 1e-6, beside which the borders of
 // a sampled token lie close.
 //
-// One workgroup takes a request: its walk looks at single probabilities, which it has read at once into
+// A workgroup takes a request: its walk looks at single probabilities, which it has read at once into
 // the LDS, and a pass over a row sums r where a rejected child has a sibling after it or the token is
 // to be sampled. A pass is bound by the vector instructions of its compute unit, 9 for an element (two
-// conversions and three operations in fp64, the check of its bits): 100003 tokens about 6 us. A pass
-// shared by several workgroups would exchange its sum through memory, four trips of 0.7 us, and gain
-// from about 200 thousand tokens on. 32 trees of up to 25 nodes over 100003 tokens: 47 us, as long as the
-// request with the most rejections.
+// conversions and three operations in fp64, the check of its bits): 100003 tokens about 6 us. So
+// other workgroups help where few requests leave the GPU idle: each sums its parts of the row for the
+// passes that it is told of, through memory, in about 4 us with all trips. 32 trees of up to 25 nodes over
+// 100003 tokens: 33 us (47 us alone), as long as the request with the most rejections takes.
 #include "draft.h"
 #include "qcache_ops.h"
 
@@ -528,11 +528,14 @@ __global__ __launch_bounds__(kThreads, kGroups * kWaves / 4) void verify_kernel(
 
 }  // namespace
 
-// Workgroups of a request: as many as run together, none without a part of the row.
+// Workgroups of a request: as many as run together, none without a part of the row, where the row has four parts
+// and eight or more run together. (Trees of 16 over 200000 tokens, bf16: one request 35.5 us alone, 14.9
+// shared, 32 of them 91 and 36; 32 over 32768 tokens 23.7 and 20.7, over 16384 17.5 and 20.1; with four
+// workgroups each, 128 requests over 32768 tokens 19.7 and 23.4, over 50000 27.1 and 29.3.)
 int32_t verify_groups(int32_t n, int64_t V) {
   const int64_t part = (V + kParts * kPart - 1) / (kParts * kPart) * kPart, parts = (V + part - 1) / part;
   const int64_t groups = (int64_t)kGroups * device_cu_count() / n;
-  return (int32_t)(groups < 1 ? 1 : groups > parts ? parts : groups);
+  return (int32_t)(groups < 8 || parts < 4 ? 1 : groups > parts ? parts : groups);
 }
 size_t verify_workspace(int32_t n, int64_t V) {
   return verify_groups(n, V) > 1 ? sizeof(VerifyTalk) * (size_t)n : 0;

@@ -8,6 +8,7 @@ the current one), marks the tensors it was given as in use there and does not wa
 from __future__ import annotations
 
 import ctypes
+import functools
 from dataclasses import dataclass
 from typing import Optional
 
@@ -216,17 +217,25 @@ def verify_drafts(probs: torch.Tensor, drafts: torch.Tensor, parents: torch.Tens
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _verify_bytes(dev, n: int, dtype: int, vocabulary: int) -> int:
+    """The workspace of these sizes on the current GPU, dev."""
+    need = ctypes.c_size_t(0)
+    step = C.CmDrafts(n=n, dtype=dtype, vocabulary=vocabulary)
+    C.check(C.lib().cm_verify_drafts_size(ctypes.byref(step), ctypes.byref(need)), "cm_verify_drafts_size")
+    return need.value
+
+
 def _verify_workspace(step: C.CmDrafts, dev, s) -> Optional[torch.Tensor]:
     """Zeros for a call on s, the current stream; kept as the attention's scratch is."""
-    need = ctypes.c_size_t(0)
-    C.check(C.lib().cm_verify_drafts_size(ctypes.byref(step), ctypes.byref(need)), "cm_verify_drafts_size")
-    if need.value == 0:
+    need = _verify_bytes(dev, step.n, step.dtype, step.vocabulary)
+    if need == 0:
         return None
     capturing = torch.cuda.is_current_stream_capturing()
     key = (dev, s.cuda_stream, "cm_verify_drafts")
     ws = None if capturing else _WS.get(key)
-    if ws is None or ws.numel() < need.value:
-        ws = torch.zeros(need.value, dtype=torch.uint8, device=dev)
+    if ws is None or ws.numel() < need:
+        ws = torch.zeros(need, dtype=torch.uint8, device=dev)
         if not capturing:
             _WS[key] = ws
     return ws

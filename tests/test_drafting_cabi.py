@@ -98,6 +98,24 @@ def test_drafts_refused(lib, over, code):
     assert lib.cm_verify_drafts(None, None) == C.CM_EINVAL
 
 
+def test_drafts_workspace(lib):
+    def size(**over):
+        n = ctypes.c_size_t(7)
+        return lib.cm_verify_drafts_size(ref(drafts(**over)), ref(n)), n.value
+
+    assert size(n=1024, vocabulary=200_000) == (C.CM_OK, 0) and size(vocabulary=1000) == (C.CM_OK, 0)
+    assert size(n=0)[0] == C.CM_EINVAL and size(dtype=7)[0] == C.CM_EDTYPE and size(vocabulary=0)[0] == C.CM_EINVAL
+    assert lib.cm_verify_drafts_size(None, ref(ctypes.c_size_t(0))) == C.CM_EINVAL
+    assert lib.cm_verify_drafts_size(ref(drafts()), None) == C.CM_EINVAL
+    # misaligned, whatever is needed
+    need = size(n=2, vocabulary=200_000)[1]
+    if need:
+        for at, some in ((0xb00010, need), (0xb00000, need - 1)):
+            wrong = drafts(n=2, vocabulary=200_000, probs_stride=200_000, draft_probs_stride=200_000, workspace=at,
+                           workspace_bytes=some)
+            assert lib.cm_verify_drafts(ref(wrong), None) == C.CM_EWORKSPACE
+
+
 def cache(**over):
     f = dict(L=2, H=4, d=128, block=16, pages=100, codes_dev=0x100000, scales_dev=0x200000)
     f.update(over)
