@@ -37,7 +37,7 @@ constexpr int kStep = 64 * kVec;     // and of a wave's
 // for a pass, the first one for the helpers' sums. Neither is needed: a helper that has waited this long
 // ends, and the first one makes the sums itself.
 constexpr uint64_t kHelperWait = 100000;
-constexpr uint64_t kSumsWait = 20000;
+constexpr uint64_t kSumsWait = 3000;
 
 // What is not a probability counts as none.
 __device__ __forceinline__ double clean(float x) {
