@@ -1,4 +1,4 @@
-// Internal interface of the operators for drafted decoding (norm_rotate.hip, draft_*.hip).
+// Internal interface of the operators for drafted decoding (norm_rotate.hip, qcache_tree.hip, verify.hip, qcache_keep.hip).
 #pragma once
 
 #include "qcache.h"
