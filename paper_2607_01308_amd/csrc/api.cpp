@@ -1240,6 +1240,7 @@ struct Range {
   const char* name;
 };
 bool overlap(const Range& x, const Range& y) {
+  if (x.bytes == 0 || y.bytes == 0) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
   return a < b + (uintptr_t)y.bytes && b < a + (uintptr_t)x.bytes;
 }
