@@ -716,7 +716,9 @@ int32_t cm_qcache_tree_attention(const cm_qcache* cache, int32_t layer, const cm
  * path_dev, at the request's rows: the numbers of the accepted nodes in order, 0 first, -1 behind
  * them; counts_dev[r]: how many. A request without nodes, with more than CM_DRAFT_MAX_NODES, or whose
  * rows do not lie in order in [0, n_rows] has count 0 and token -1; rows of no request are left as
- * they are. A parent that is no earlier node of the request makes the node nobody's child. */
+ * they are. A parent that is no earlier node of the request makes the node nobody's child.
+ * path_dev, counts_dev, tokens_dev and the workspace overlap nothing else of the call (a row of
+ * probabilities goes on to where the next one begins). */
 typedef struct {
   int32_t n;                       /* requests, at most CM_QCACHE_MAX_REQUESTS */
   int32_t dtype;                   /* cm_dtype of the probabilities */

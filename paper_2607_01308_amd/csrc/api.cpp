@@ -1682,6 +1682,28 @@ int32_t cm_verify_drafts(const cm_drafts* s, void* stream) {
   if (s->workspace &&
       (st = check_ws(s->workspace, s->workspace_bytes, cm::verify_workspace(s->n, s->vocabulary))) != CM_OK)
     return st;
+  // several workgroups take a request: what one writes another may still have to read
+  const auto extent = [&](int64_t stride) {
+    const double bytes = ((double)(s->n_rows - 1) * stride + (double)s->vocabulary) * esize;
+    return bytes > 0x1p62 ? (int64_t)1 << 62 : ((s->n_rows - 1) * stride + s->vocabulary) * esize;
+  };
+  const int64_t n = s->n, rows = s->n_rows,
+                ws_bytes = s->workspace ? (int64_t)cm::verify_workspace(s->n, s->vocabulary) : 0;
+  const Range written[] = {{s->path_dev, 4 * rows, "path_dev"}, {s->counts_dev, 4 * n, "counts_dev"},
+                           {s->tokens_dev, 8 * n, "tokens_dev"}, {s->workspace, ws_bytes, "workspace"}};
+  const Range read[] = {{s->probs_dev, rows ? extent(rows > 1 ? s->probs_stride : 0) : 0, "probs_dev"},
+                        {s->draft_probs_dev,
+                         rows && s->draft_probs_dev ? extent(rows > 1 ? s->draft_probs_stride : 0) : 0, "draft_probs_dev"},
+                        {s->drafts_dev, 8 * rows, "drafts_dev"}, {s->parents_dev, 4 * rows, "parents_dev"},
+                        {s->rows_dev, 4 * (n + 1), "rows_dev"}, {s->accept_dev, 4 * rows, "accept_dev"},
+                        {s->sample_dev, 4 * n, "sample_dev"}};
+  for (const Range& w : written) {
+    for (const Range& r : read)
+      if (overlap(w, r)) return fail(CM_EINVAL, std::string(w.name) + " overlaps " + r.name);
+    for (const Range& other : written)
+      if (&other > &w && overlap(w, other))
+        return fail(CM_EINVAL, std::string(w.name) + " overlaps " + other.name);
+  }
   cm::VerifyArgs a;
   a.talk = s->workspace;
   a.n = s->n;
