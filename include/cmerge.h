@@ -685,7 +685,10 @@ int32_t cm_qcache_tree(int32_t n, int64_t n_rows, const int32_t* parents_dev, co
  * window: if j > positions - window, positions that of the row, in [held, held + c)) and the place
  * held + j, 0 <= j < c, if bit j of its mask is set. Places whose table entry is not a page in
  * [0, P) are hidden, and so are those below 0. Masks may be any, not only those of trees; a mask
- * without bits leaves the context alone. Rows past max_rows are not computed; their nodes' K and V
+ * without bits leaves the context alone. What a row does not see has no effect on it, scales included;
+ * a row that sees a token whose K or V has a scale that is not finite is NaN, and where it is K's its lse too.
+ * Weights are relative to an earlier maximum and may be up to 2^8: sums of V's values times that stay
+ * below 2^128. Rows past max_rows are not computed; their nodes' K and V
  * are seen by those whose masks say so. A request whose rows do not lie in order in [0, n_rows] has
  * none. Workspace: cm_qcache_tree_attention_size() bytes, under the same rules as
  * cm_qcache_attention's, whose workspace it may share. */

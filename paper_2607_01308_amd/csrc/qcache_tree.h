@@ -146,6 +146,7 @@ struct TreeShared {
     float acc[kTreeWaves][16 * kTogether][D + 4];              // the waves' results
   };
   float m[kTreeWaves][16 * R], l[kTreeWaves][16 * R];
+  uint32_t spoilt[kTreeWaves][16 * R];                         // rows that see a scale that is not finite: 1 V's, 2 K's
   int pos[CM_QCACHE_MAX_REQUESTS + 1];                         // where the requests begin, in units
   float cost[kTreeWaves];
   int sums[kTreeWaves], tiles[kTreeWaves];
@@ -279,26 +280,43 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
   uint8_t* staged = lds.codes[wave];
   constexpr int kPieces = D / 16;                // of a token
   const uint32_t put = code_place<D>(lane / kPieces, lane % kPieces), lane_at = lane * 16;
+  if (lane < 16 * R) lds.spoilt[wave][lane] = 0;
   // 64 tiles of 16 tokens at a time: their pages and scales, one lane each
   for (int t0 = begin; t0 < end; t0 += 64 * 16) {
     int32_t my_page = 0;
     // (not 0, also where the softmax scale is: hidden scores are -inf times it)
     float my_ks = 0x1p-126f, my_vs = 1.f;
     const int my_t = t0 + lane * 16;
-    bool there = false;
+    bool there = false, k_odd = false, v_odd = false;
     if (my_t < end) {
       my_page = table[my_t >> a.b_shift];
       there = my_page >= 0 && my_page < a.pages;
       if (!there) my_page = 0;
-      my_ks = fmaxf(a.ks[(int64_t)my_page * a.H + h] * a.scale_log2, 0x1p-126f);
-      if (there) my_vs = a.vs[(int64_t)my_page * a.H + h];
+      const float ks = a.ks[(int64_t)my_page * a.H + h] * a.scale_log2;
+      const float vs = a.vs[(int64_t)my_page * a.H + h];
+      k_odd = there && !(ks < __builtin_inff());
+      v_odd = there && !(vs < __builtin_inff());
+      if (ks < __builtin_inff()) my_ks = fmaxf(ks, 0x1p-126f);
+      if (there && vs < __builtin_inff()) my_vs = vs;
+    }
+    // (the products, which all rows share, take other scales in their place)
+    if (__builtin_expect(__any(k_odd || v_odd), 0)) {
+      const uint64_t k_tiles = __ballot(k_odd), v_tiles = __ballot(v_odd);
+      for (uint64_t tiles = k_tiles | v_tiles; tiles; tiles &= tiles - 1) {
+        const int tile = __builtin_ctzll(tiles), row = lane_anew();
+        if (row < 16 * R && (tree_sees(ta, it, (rho0 + row) / a.G, t0 + tile * 16) & 0xFFFFu))
+          lds.spoilt[wave][row] |= ((v_tiles >> tile) & 1) | ((k_tiles >> tile) & 1) << 1;
+      }
     }
     // V's scale as a power of two, which the conversion of its codes takes, times a rest in [1, 2),
     // which the weights' exponent takes; their sum is divided by it. (An exponent field of 0 stands for
-    // 2^-127 in the conversion; a scale of 0 is that.)
-    const uint32_t vs_exponent = __float_as_uint(my_vs) & 0x7F800000u;
+    // 2^-127 in the conversion; a scale of 0 is that. Beyond 2^119 the greatest codes would be infinite,
+    // and NaN times the weight 0 of a row that does not see them: the rest takes what is above it.)
+    const uint32_t vs_field = __float_as_uint(my_vs) & 0x7F800000u;
+    const uint32_t vs_exponent = vs_field < 0x7B000000u ? vs_field : 0x7B000000u;
     const float my_vp = __uint_as_float(vs_exponent);
-    const float rest = vs_exponent ? __uint_as_float((__float_as_uint(my_vs) & 0x7FFFFFu) | 0x3F800000u)
+    const float rest = vs_field > vs_exponent ? my_vs * 0x1p-119f
+                       : vs_exponent ? __uint_as_float((__float_as_uint(my_vs) & 0x7FFFFFu) | 0x3F800000u)
                        : my_vs == 0.f ? 1.f : fabsf(my_vs) * 0x1p127f;
     const float my_vl = __builtin_amdgcn_logf(rest), my_vi = 1.f / rest;
     const uint64_t absent = ~__ballot(there);
@@ -548,12 +566,14 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
   // the waves' results as one, by all threads, kTogether row tiles at a time
   constexpr int kTogether = TreeShared<TERMS, D, R>::kTogether;
   const int en = anew(n), eg = anew(g);
+  uint32_t spoilt[R];
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     const float sum = lane_sum<32>(lane_sum<16>(l[j]));
+    spoilt[j] = lds.spoilt[wave][16 * j + en];
     if (eg == 0) {
       lds.m[wave][16 * j + en] = ref[j];
-      lds.l[wave][16 * j + en] = sum;
+      lds.l[wave][16 * j + en] = spoilt[j] & 2 ? __builtin_nanf("") : sum;
     }
   }
   const int live = it.count * a.G - rho0;        // rows of the tile that there are
@@ -566,6 +586,9 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
       float* row = &lds.acc[wave][16 * jj + en][4 * eg];
 #pragma unroll
       for (int c = 0; c < DW; ++c) *reinterpret_cast<f32x4*>(&row[16 * c]) = acc[j0 + jj][c];
+      if (__builtin_expect(spoilt[j0 + jj] != 0, 0))
+#pragma unroll
+        for (int c = 0; c < DW; ++c) *reinterpret_cast<f32x4*>(&row[16 * c]) = f32x4{} + __builtin_nanf("");
     }
     __syncthreads();
     constexpr int kQuads = D / 4;
