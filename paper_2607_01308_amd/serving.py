@@ -138,16 +138,22 @@ class ServingCache:
             if any(not 0 <= p < i for i, p in enumerate(tree) if i) or tree[:1] not in ((), (-1,)):
                 raise ValueError(f"place {r}: node 0 hangs on -1, every other on an earlier one, got "
                                  f"{list(tree)}")
-        if window < 0:
-            raise ValueError(f"window must be >= 0, got {window}")
+        if not 0 <= window < 2 ** 31:
+            raise ValueError(f"window must be in [0, 2^31), got {window}")
+        before = self._head, self._held, self.lengths
         step = self.extend([len(tree) for tree in parents], stream)
-        if self._parents is None or self._parents[0] != parents:
-            self._parents = (parents, *self._upload([p for tree in parents for p in tree], stream))
-        elif self._held.is_cuda:
-            _use(stream, self._held.device, self._parents[1])
-        step.parents = self._parents[1]
-        step.tree = qcache_tree(step.parents, step.tables.rows, step.tables.lens, step.tokens,
-                                step.max_rows, window, stream=stream)
+        try:
+            if self._parents is None or self._parents[0] != parents:
+                self._parents = (parents, *self._upload([p for tree in parents for p in tree], stream))
+            elif self._held.is_cuda:
+                _use(stream, self._held.device, self._parents[1])
+            step.parents = self._parents[1]
+            step.tree = qcache_tree(step.parents, step.tables.rows, step.tables.lens, step.tokens,
+                                    step.max_rows, window, stream=stream)
+        except Exception:
+            # (as in load: the pages are dealt again)
+            self._head, self._held, self.lengths = before
+            raise
         return step
 
     def _upload(self, numbers: Sequence[int], stream):

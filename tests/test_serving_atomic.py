@@ -1,0 +1,69 @@
+"""Steps of ServingCache that fail leave nothing changed, and steps that cannot be are refused before anything
+is, on the CPU with the plain stand-ins of test_serving_drafts.py."""
+
+import pytest
+import torch
+
+from paper_2607_01308_amd import serving
+from test_serving import plain  # noqa: F401
+from test_serving_drafts import cache_of, check, numbers  # noqa: F401
+
+
+def state(sc):
+    return list(sc.lengths), sc.free_pages, sc._held.tolist(), [list(x) for x in sc._shared]
+
+
+def grown(sc):
+    """Place 0 with 20 tokens, which the stand-in's pages hold."""
+    step = sc.extend([20] + [0] * (sc.places - 1))
+    for i, slot in enumerate(step.tables.slots.tolist()):
+        sc.cache.tokens[slot // sc.cache.B, slot % sc.cache.B] = i
+    return [list(range(20))] + [[] for _ in range(sc.places - 1)]
+
+
+@pytest.mark.parametrize("part", ["qcache_tree", "upload"])
+def test_a_draft_that_fails_changes_nothing(numbers, monkeypatch, part):  # noqa: F811
+    sc = cache_of(10, 16, 2, 100)
+    want = grown(sc)
+    before = state(sc)
+
+    def refuse(*args, **kwargs):
+        raise RuntimeError("refused")
+
+    with monkeypatch.context() as m:
+        if part == "upload":
+            m.setattr(sc, "_upload", refuse)
+        else:
+            m.setattr(serving, "qcache_tree", refuse)
+        for _ in range(3):
+            with pytest.raises(RuntimeError, match="refused"):
+                sc.draft([[-1] + [0] * 20, [-1]])
+            assert state(sc) == before
+    check(sc, want)
+    step = sc.draft([[-1, 0], []])
+    assert sc.lengths == [22, 0] and step.tokens == 2
+
+
+@pytest.mark.parametrize("window", [-1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63])
+def test_windows_of_no_32_bits(numbers, window):  # noqa: F811
+    sc = cache_of(10, 16, 2, 100)
+    grown(sc)
+    before = state(sc)
+    with pytest.raises(ValueError, match="window"):
+        sc.draft([[-1, 0], []], window=window)
+    assert state(sc) == before
+    sc.draft([[-1, 0], []], window=2 ** 31 - 1)
+
+
+def test_counts_and_parents_that_are_no_numbers(numbers):  # noqa: F811
+    sc = cache_of(10, 16, 2, 100)
+    grown(sc)
+    before = state(sc)
+    with pytest.raises((TypeError, ValueError)):
+        sc.draft([["a"], []])
+    assert state(sc) == before
+    step = sc.draft([[-1, 0], []])
+    after = state(sc)
+    with pytest.raises((TypeError, ValueError)):
+        sc.accept(step, torch.zeros(2, dtype=torch.int32), [None, 0])
+    assert state(sc) == after
