@@ -16,7 +16,7 @@ import torch
 
 from . import _cabi as C
 from .binding import _DTYPES, _STYLES
-from .qcache import _WS, QCache, _attention, _attention_step, _call, _check, _made_on, _use
+from .qcache import _WS, QCache, _attention, _attention_step, _call, _check, _int32, _made_on, _use
 
 
 def _heads(x: torch.Tensor, out: Optional[torch.Tensor], weight: Optional[torch.Tensor], name: str,
@@ -116,7 +116,8 @@ def qcache_tree(parents: Optional[torch.Tensor], rows: torch.Tensor, lens: torch
     _check(rows, "rows", torch.int32, dev, (n + 1,))
     if parents is not None:
         _check(parents, "parents", torch.int32, dev, (tokens,))
-    words = -(-max(max_rows, 1) // 64) if masks else 0
+    words = -(-_int32(max(max_rows, 1), "max_rows") // 64) if masks else 0
+    window = _int32(window, "window")
     with _made_on(stream):
         out = QCacheTree(torch.empty((tokens, words), dtype=torch.int64, device=dev) if masks else None,
                          torch.empty(tokens, dtype=torch.int32, device=dev), window,
@@ -301,6 +302,6 @@ def qcache_copy(cache: QCache, src: torch.Tensor, dst: torch.Tensor, layer: int 
     _check(src, "src", torch.int32, cache.device)
     _check(dst, "dst", torch.int32, cache.device, src.shape)
     s, here = _use(stream, cache.device, cache.codes, cache.scales, src, dst)
-    C.check(_call(here, cache.device, C.lib().cm_qcache_copy, ctypes.byref(cache.struct), layer,
-                  cache.L - layer if layers is None else layers, src.numel(), src.data_ptr(),
-                  dst.data_ptr(), s.cuda_stream), "cm_qcache_copy")
+    C.check(_call(here, cache.device, C.lib().cm_qcache_copy, ctypes.byref(cache.struct),
+                  _int32(layer, "layer"), _int32(cache.L - layer if layers is None else layers, "layers"),
+                  src.numel(), src.data_ptr(), dst.data_ptr(), s.cuda_stream), "cm_qcache_copy")

@@ -85,6 +85,13 @@ def _call(here: bool, device, f, *args) -> int:
         return f(*args)
 
 
+def _int32(x: int, name: str) -> int:
+    """A number that the library takes in 32 bits (ctypes would cut it to them)."""
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{name} must be a number of 32 bits, got {x}")
+    return x
+
+
 def _check(t: torch.Tensor, name: str, dtype, device, shape=None) -> torch.Tensor:
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
@@ -141,7 +148,7 @@ def qcache_tables(pages: int, block: int, held: torch.Tensor, new: torch.Tensor,
                           torch.empty(4, dtype=torch.int64, device=dev))
     s, here = _use(stream, dev, held, new, free, table)
     C.check(_call(here, dev, C.lib().cm_qcache_tables,
-                  pages, block, n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
+                  pages, _int32(block, "block"), n, held.data_ptr(), new.data_ptr(), free.data_ptr(), free.numel(),
                   table.data_ptr(), width, tokens, step.slots.data_ptr(), step.rows.data_ptr(),
                   step.lens.data_ptr(), step.info.data_ptr(), s.cuda_stream), "cm_qcache_tables")
     return step
@@ -187,8 +194,8 @@ def qcache_write(cache: QCache, layer: int, k: torch.Tensor, v: torch.Tensor,
     if layers != v_layers:
         raise ValueError("k and v must have the same layers")
     s, here = _use(stream, cache.device, cache.codes, cache.scales, k, v, slots)
-    C.check(_call(here, cache.device, C.lib().cm_qcache_write, ctypes.byref(cache.struct), layer,
-                  layers, _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens,
+    C.check(_call(here, cache.device, C.lib().cm_qcache_write, ctypes.byref(cache.struct),
+                  _int32(layer, "layer"), layers, _DTYPES[k.dtype], ctypes.byref(kr), ctypes.byref(vr), tokens,
                   slots.data_ptr(), s.cuda_stream), "cm_qcache_write")
 
 
@@ -242,7 +249,7 @@ def _attention_step(cache: QCache, q, table, lens, rows, max_rows, scale, window
         raise ValueError("out must have q's shape, type and device and a contiguous last dimension")
     _check(lse, "lse", torch.float32, dev, (n_rows, q_heads))
     step = C.CmQattention(
-        n, q_heads, _DTYPES[q.dtype], window, n_rows, max_rows,
+        n, q_heads, _DTYPES[q.dtype], _int32(window, "window"), n_rows, _int32(max_rows, "max_rows"),
         d ** -0.5 if scale is None else scale, q.data_ptr(), q.stride(0), q.stride(1),
         out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
         None if rows is None else rows.data_ptr(), lens.data_ptr(), table.data_ptr(), width)
@@ -280,6 +287,7 @@ def _attention(cache: QCache, layer: int, step: C.CmQattention, s, call: str = "
     be replaced while the graph still refers to it."""
     capturing = torch.cuda.is_current_stream_capturing()
     key = (cache.device, s.cuda_stream)
+    layer = _int32(layer, "layer")
     size = call + "_size"
     ws = _workspace(cache, step, size) if capturing else _WS.get(key, _NONE)
     args = ctypes.byref(cache.struct), layer, ctypes.byref(step), *more
