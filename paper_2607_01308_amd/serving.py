@@ -31,7 +31,7 @@ import torch
 
 from ._cabi import CM_DRAFT_MAX_NODES
 from .binding import _DTYPES
-from .drafting import QCacheTree, qcache_copy, qcache_keep, qcache_tree, qcache_tree_attention
+from .drafting import QCacheKept, QCacheTree, qcache_copy, qcache_keep, qcache_tree, qcache_tree_attention
 from .qcache import (QCache, QCacheStep, _made_on, _use, check_rows, qcache_attention,
                      qcache_tables, qcache_write)
 
@@ -169,10 +169,11 @@ class ServingCache:
         return qcache_tree(None, step.tables.rows, step.tables.lens, step.tokens, step.max_rows,
                            masks=False, stream=stream).positions
 
-    def accept(self, step: ServingStep, path: torch.Tensor, counts: Sequence[int], stream=None) -> None:
+    def accept(self, step: ServingStep, path: torch.Tensor, counts: Sequence[int], stream=None) -> QCacheKept:
         """Of the nodes of a drafted step, the last one, the first counts[r] of place r's path (as
         verify_drafts gives it) stay, and their K and V move to the front; the others' pages are
-        free again."""
+        free again. The path stays on the device: check() of what this returns waits and raises where one
+        was not ascending within the nodes, of whose place nothing has moved then."""
         self._refuse_capture("accept", stream)
         counts = tuple(int(x) for x in counts)
         if step.tables.lens is not self._held:
@@ -190,6 +191,7 @@ class ServingCache:
                            self._free[self._tail:self._tail + pages], stream)
         self._tail += pages
         self._held, self.lengths = kept.lens, after
+        return kept
 
     def fork(self, place: int, to: int, stream=None) -> None:
         """The empty place `to` goes on from the tokens of `place`: both hold the same full pages,

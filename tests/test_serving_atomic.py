@@ -67,3 +67,22 @@ def test_counts_and_parents_that_are_no_numbers(numbers):  # noqa: F811
     with pytest.raises((TypeError, ValueError)):
         sc.accept(step, torch.zeros(2, dtype=torch.int32), [None, 0])
     assert state(sc) == after
+
+
+def test_accept_tells_what_became_of_the_path(numbers, monkeypatch):  # noqa: F811
+    """The status that the library leaves on the device is the caller's to ask for."""
+    from paper_2607_01308_amd._cabi import CmError
+    from paper_2607_01308_amd.drafting import QCacheKept
+
+    sc = cache_of(10, 16, 2, 100)
+    grown(sc)
+    step = sc.draft([[-1, 0, 0], [-1]])
+    kept = sc.accept(step, torch.tensor([0, 2, -1, 0], dtype=torch.int32), [2, 1])
+    assert kept.check() is kept and kept.lens.tolist() == sc.lengths == [22, 1]
+    assert kept.info.tolist() == [0, 0]
+
+    bad = QCacheKept(torch.zeros(2, dtype=torch.int32), torch.tensor([2, 0]))
+    step = sc.draft([[-1, 0, 0], []])
+    monkeypatch.setattr(serving, "qcache_keep", lambda *a, **k: bad)
+    with pytest.raises(CmError, match="path"):
+        sc.accept(step, torch.tensor([0, 2, 1], dtype=torch.int32), [3, 0]).check()
