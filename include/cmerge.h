@@ -652,7 +652,7 @@ typedef struct {
  *   pair i of y turned by the angle positions_dev[t] * base^(-2i/d): (a, b) becomes
  *   (a cos - b sin, b cos + a sin); the pairs as rope->style says
  * Angles are reduced in fp64, norms and products are in fp32, a result is rounded once to
- * dtype (of the rows, cm_dtype). A row whose sum of squares leaves the range of fp32 gives
+ * dtype (of the rows, cm_dtype). A row whose sum of squares is above the range of fp32 gives
  * zeros. positions_dev: n_tokens int32, any values. d is 64, 128 or 256. */
 int32_t cm_norm_rotate(int32_t d, int32_t dtype, int64_t n_tokens, const int32_t* positions_dev,
                        const cm_rope* rope, float eps, const cm_head_rows* q, const cm_head_rows* k,

@@ -153,12 +153,26 @@ __global__ __launch_bounds__(kThreads, kGroups) void norm_rotate_kernel(RotateAr
       unpack<ES>(*global_ptr<u32x4>(in), x[0]);
       unpack<ES>(*global_ptr<u32x4>(in + D / 2 * ES), x[1]);
       if (is_k ? a.k.weight != nullptr : a.q.weight != nullptr) {
-        float sum = 0.f;
+        const auto squares = [&] {
+          float sum = 0.f;
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int e = 0; e < E; ++e) sum = fmaf(x[s][e], x[s][e], sum);
-        const float inv = 1.f / sqrtf(row_sum<kLanes>(sum) * (1.f / D) + a.eps);
+            for (int e = 0; e < E; ++e) sum = fmaf(x[s][e], x[s][e], sum);
+          return row_sum<kLanes>(sum);
+        };
+        float sum = squares(), eps = a.eps;
+        // (rows whose squares leave the range of fp32 downwards, times 2^96, where eps does not cover that)
+        if (a.eps < 0x1p-66f && __any(sum < 0x1p-96f)) {
+          const float up = sum < 0x1p-96f ? 0x1p96f : 1.f;
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[s][e] *= up;
+          sum = squares();
+          eps = eps * up * up;
+        }
+        const float inv = 1.f / sqrtf(sum * (1.f / D) + eps);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
