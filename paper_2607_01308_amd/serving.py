@@ -250,19 +250,23 @@ class ServingCache:
         # the table's entries whose pages nobody else holds
         runs, at = [], 0
         for run in self._shared[place]:
-            run.places -= 1
-            if run.places == 0:
+            if run.places == 1:
                 runs.append((at, at + run.pages))
             at += run.pages
-        self._shared[place] = []
         runs.append((at, pages))
         self._room(pages, stream)
+        tail = self._tail
         with _made_on(stream):
+            held = self._held.clone()                     # (a step may still be read)
+            held[place:place + 1].zero_()
             for a, b in runs:
-                self._free[self._tail:self._tail + b - a] = self.table[place, a:b]
-                self._tail += b - a
-            self._held = self._held.clone()               # (a step may still be read)
-            self._held[place:place + 1].zero_()
+                self._free[tail:tail + b - a] = self.table[place, a:b]
+                tail += b - a
+        # (nothing fails from here on)
+        for run in self._shared[place]:
+            run.places -= 1
+        self._shared[place] = []
+        self._tail, self._held = tail, held
         self.lengths[place] = 0
 
     def write(self, layer: int, k: torch.Tensor, v: torch.Tensor, step: ServingStep,

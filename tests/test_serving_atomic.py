@@ -86,3 +86,61 @@ def test_accept_tells_what_became_of_the_path(numbers, monkeypatch):  # noqa: F8
     monkeypatch.setattr(serving, "qcache_keep", lambda *a, **k: bad)
     with pytest.raises(CmError, match="path"):
         sc.accept(step, torch.tensor([0, 2, 1], dtype=torch.int32), [3, 0]).check()
+
+
+class Failing:
+    """torch functions that fail from the n-th call on."""
+    def __init__(self, real, after):
+        self.real, self.left = real, after
+
+    def __call__(self, *args, **kwargs):
+        self.left -= 1
+        if self.left < 0:
+            raise RuntimeError("out of memory")
+        return self.real(*args, **kwargs)
+
+
+@pytest.mark.parametrize("what", ["release", "fork", "accept", "extend"])
+@pytest.mark.parametrize("after", [0, 1, 2])
+def test_steps_without_memory_change_nothing(numbers, monkeypatch, what, after):  # noqa: F811
+    """Whatever allocation of a step fails: lengths, pages and who shares them are as before, and the step can
+    be taken again."""
+    sc = cache_of(14, 16, 3, 100)
+    want = grown(sc)
+    sc.fork(0, 1)
+    want[1] = list(want[0])
+    step = sc.draft([[-1, 0, 1] + [0] * 20, [], []])
+    ids = [100 + i for i in range(23)]
+    for slot, x in zip(step.tables.slots.tolist(), ids):
+        sc.cache.tokens[slot // 16, slot % 16] = x
+    if what != "accept":
+        sc.accept(step, torch.tensor([0, 1, 2] + [-1] * 20, dtype=torch.int32), [3, 0, 0])
+        want[0] = want[0] + ids[:3]
+        # (the buffer of free pages is to be moved to its front by the next release)
+        for _ in range(3):
+            sc.extend([0, 0, 60])
+            sc.release(2)
+    calls = {"release": lambda: sc.release(0), "fork": lambda: sc.fork(0, 2), "extend": lambda: sc.extend([5, 0, 2]),
+             "accept": lambda: sc.accept(step, torch.tensor([0, 1, 2] + [-1] * 20, dtype=torch.int32), [3, 0, 0])}
+    before, runs = state(sc), [[(run.pages, run.places) for run in x] for x in sc._shared]
+    failed = False
+    with monkeypatch.context() as m:
+        # (clones of tensors, and tensors from the host)
+        clone, made = Failing(torch.Tensor.clone, after), Failing(torch.tensor, after)
+        m.setattr(torch.Tensor, "clone", lambda t: clone(t))
+        m.setattr(torch, "tensor", made)
+        try:
+            calls[what]()
+        except RuntimeError:
+            failed = True
+    if not failed:
+        return
+    assert state(sc) == before and [[(run.pages, run.places) for run in x] for x in sc._shared] == runs
+    if what in ("release", "fork"):
+        check(sc, want)
+        calls[what]()
+        if what == "release":
+            want[0] = []
+        else:
+            want[2] = list(want[0])
+        check(sc, want)
