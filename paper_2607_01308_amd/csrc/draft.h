@@ -91,7 +91,13 @@ struct VerifyArgs {
   int64_t* tokens;
   void* talk;              // verify_workspace() bytes, or nullptr: one workgroup a request
   int32_t groups;          // of the launch: workgroups of a request
+  uint64_t helper_wait, sums_wait;  // and verify_waits
 };
+// How long the workgroups of a request wait for one another, in ticks of 10 ns for each 8192 elements (or
+// part of them) of a part of the row: a helper for a pass, the first one for the helpers' sums. Neither is
+// needed: a helper that has waited this long ends, and the first one makes the sums itself. With 0 nobody
+// looks; tests set them, between launches.
+extern uint64_t verify_waits[2];
 size_t verify_workspace(int32_t n, int64_t V);
 hipError_t launch_verify_drafts(VerifyArgs a, int32_t dtype, hipStream_t stream);
 

@@ -33,11 +33,6 @@ constexpr int kParts = 64;           // parts of a row at most
 constexpr int64_t kPart = 8192;      // elements of one, or a multiple
 constexpr int kVec = 8;              // elements of a lane's load
 constexpr int kStep = 64 * kVec;     // and of a wave's
-// How long a workgroup waits for another one, in ticks of 10 ns for each kPart elements of a part: a helper
-// for a pass, the first one for the helpers' sums. Neither is needed: a helper that has waited this long
-// ends, and the first one makes the sums itself.
-constexpr uint64_t kHelperWait = 100000;
-constexpr uint64_t kSumsWait = 3000;
 
 // What is not a probability counts as none.
 __device__ __forceinline__ double clean(float x) {
@@ -314,17 +309,14 @@ __global__ __launch_bounds__(kThreads, kGroups * kWaves / 4) void verify_kernel(
     uint32_t done = 0;
     while (true) {
       if (threadIdx.x == 0) {
-        const uint64_t start = wall_clock64();
-        uint64_t M, pass;
-        while (true) {
+        const uint64_t start = wall_clock64(), wait = a.helper_wait * (uint64_t)(part / kPart);
+        uint64_t M = 0, pass = kOver;
+        for (uint64_t now = start; now - start < wait; now = wall_clock64()) {
           M = told(&talk->pass[0]);
           pass = told(&talk->pass[1]);
           const bool whole = told(&talk->pass[2]) == (M ^ mark(pass));
           if (whole && (uint32_t)(pass >> 32) > done) break;
-          if (wall_clock64() - start > kHelperWait * (uint64_t)(part / kPart)) {
-            pass = kOver;
-            break;
-          }
+          pass = kOver;
           __builtin_amdgcn_s_sleep(1);
         }
         lds.M = M;
@@ -373,9 +365,9 @@ __global__ __launch_bounds__(kThreads, kGroups * kWaves / 4) void verify_kernel(
     for (int i = (int)threadIdx.x * helpers; i < parts; i += kThreads * helpers) lds.part[i] = part_sum(i);
     if (helpers > 1) {
       if (wave == 0) {
-        const uint64_t start = wall_clock64();
+        const uint64_t start = wall_clock64(), wait = a.sums_wait * (uint64_t)(part / kPart);
         bool wants = lane < parts && lane % helpers != 0;
-        while (true) {
+        for (uint64_t now = start; now - start < wait; now = wall_clock64()) {
           if (wants) {
             const uint64_t x = told(&talk->part[lane].sum);
             if (told(&talk->part[lane].mixed) == (x ^ mark(pass * kParts + lane))) {
@@ -383,7 +375,7 @@ __global__ __launch_bounds__(kThreads, kGroups * kWaves / 4) void verify_kernel(
               wants = false;
             }
           }
-          if (!__any(wants) || wall_clock64() - start > kSumsWait * (uint64_t)(part / kPart)) break;
+          if (!__any(wants)) break;
         }
         const uint64_t missing = __ballot(wants);
         if (lane == 0) lds.missing = missing;
@@ -541,7 +533,11 @@ size_t verify_workspace(int32_t n, int64_t V) {
   return verify_groups(n, V) > 1 ? sizeof(VerifyTalk) * (size_t)n : 0;
 }
 
+uint64_t verify_waits[2] = {100000, 3000};
+
 hipError_t launch_verify_drafts(VerifyArgs a, int32_t dtype, hipStream_t stream) {
+  a.helper_wait = verify_waits[0];
+  a.sums_wait = verify_waits[1];
   a.groups = a.talk ? verify_groups(a.n, a.V) : 1;
   const dim3 grid((uint32_t)(a.n * a.groups));
   ScopedTiming tm(K_VERIFY_DRAFTS, stream);
