@@ -632,8 +632,8 @@ int32_t cm_qcache_attention(const cm_qcache* cache, int32_t layer, const cm_qatt
  * Heads of queries or of keys: head h of token t starts at element t * in_token_stride +
  * h * in_head_stride of in_dev and holds d consecutive elements; its result goes to
  * out_dev in the same way. 16-byte aligned, strides multiples of 16 bytes but for that of a
- * dimension of size 1. out_dev may be in_dev with the same strides; else the two do not
- * overlap. weight_dev: d elements of weight_dtype, or NULL: these heads are
+ * dimension of size 1. out_dev may be in_dev with the same strides; else what is written
+ * overlaps nothing that is read, of the other heads neither. weight_dev: d elements of weight_dtype, or NULL: these heads are
  * not normalised. heads 0 (or a NULL pointer to this): there are none. */
 typedef struct {
   const void* in_dev;

@@ -34,7 +34,7 @@ constexpr int kTreeThreads = 64 * kTreeWaves;
 constexpr int tree_tiles_most(int terms, int d) { return terms == 1 ? (d > 128 ? 2 : 4) : (d > 128 ? 1 : 2); }
 constexpr bool tree_query_shared(int terms, int d, int tiles) { return terms * d * tiles >= 256; }
 // Workgroups of a compute unit, and steps that a wave's loads are ahead of it.
-constexpr int tree_groups(int terms, int d, int tiles) { return 2; }
+constexpr int kTreeGroups = 2;
 constexpr int tree_ahead(int terms, int d, int tiles) { return d * tiles >= 512 ? 1 : d > 128 ? 1 : 2; }
 
 // Codes of a step of 32 tokens on their way from memory, in memory's order: piece x of 16 bytes of a tile
@@ -624,7 +624,7 @@ __device__ __forceinline__ void tree_segment(const TreeAttention& ta, const Tree
 
 // The ranges of a workgroup's span, one after another.
 template <int TERMS, int D, int R>
-__global__ __launch_bounds__(kTreeThreads, tree_groups(TERMS, D, R)) void qcache_tree_kernel(TreeAttention ta) {
+__global__ __launch_bounds__(kTreeThreads, kTreeGroups) void qcache_tree_kernel(TreeAttention ta) {
   __shared__ TreeShared<TERMS, D, R> lds;
   constexpr int ES = TERMS == 1 ? 2 : 4;
   constexpr int kPer = CM_QCACHE_MAX_REQUESTS / kTreeThreads;

@@ -83,7 +83,7 @@ TreePlan plan_qcache_tree(int32_t H, int32_t d, int32_t G, int32_t n, int64_t n_
   p.tiles = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
   p.tiles = p.tiles < most ? p.tiles : most;
   // workgroups that run together
-  const int64_t groups = (int64_t)tree_groups(terms, d, p.tiles) * device_cu_count();
+  const int64_t groups = (int64_t)kTreeGroups * device_cu_count();
   p.items = (int32_t)(groups / H > 0 ? groups / H : 1);
   p.places = 2 * p.items;                        // a span's first and last range
   // all contexts together, a request's once for each of its tiles, are less than 2e9 units

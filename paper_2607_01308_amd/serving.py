@@ -196,7 +196,8 @@ class ServingCache:
     def fork(self, place: int, to: int, stream=None) -> None:
         """The empty place `to` goes on from the tokens of `place`: both hold the same full pages,
         which are free again when the last of their places is released, and `to` a copy of a page
-        that is not full."""
+        that is not full, as far as it is written when the call comes to run: a step's K and V go in before
+        it is forked."""
         for x in (place, to):
             if not 0 <= x < self.places:
                 raise ValueError(f"place must be in [0, {self.places}), got {x}")
